@@ -14,7 +14,7 @@ from typing import Optional
 import numpy as np
 
 from . import _abi
-from ._abi import (OT_BF16, OT_E_CLOSED, OT_E_INVAL, OT_E_STATE, OT_EMPTY, OT_FP32, OT_NOT_READY, OT_OK,
+from ._abi import (OT_ADAPTERS_RELU, OT_ADAPTERS_RELU_INPUT, OT_BF16, OT_E_CLOSED, OT_E_INVAL, OT_E_STATE, OT_EMPTY, OT_FP32, OT_NOT_READY, OT_OK,
                    OT_POLICY_FIFO, OT_POLICY_FIRO, OT_POLICY_RESERVOIR, OT_SURROGATE_KEEP_GRADS, OTError,
                    check, last_error, load)
 
@@ -24,7 +24,10 @@ __all__ = [
     "reservoir_destroy", "surrogate_create", "surrogate_set_params", "surrogate_get_params",
     "surrogate_get_grads", "surrogate_get_adam_state", "surrogate_set_lr", "surrogate_train_step",
     "surrogate_predict", "surrogate_predict_noalloc", "surrogate_eval_loss", "surrogate_checkpoint", "surrogate_restore",
-    "reservoir_checkpoint", "reservoir_restore", "surrogate_destroy", "load", "last_error", "OTError",
+    "reservoir_checkpoint", "reservoir_restore", "surrogate_destroy", "LowRankAdapters", "GradientClip", "AdamTensors",
+    "adapters_create", "adapters_forward", "adapters_backward", "adapters_destroy", "clip_create", "clip_norm",
+    "clip_apply", "clip_destroy", "adam_create", "adam_step", "adam_set_lr", "adam_get_steps", "adam_set_steps",
+    "adam_destroy", "OT_ADAPTERS_RELU", "OT_ADAPTERS_RELU_INPUT", "load", "last_error", "OTError",
     "OT_OK", "OT_NOT_READY", "OT_EMPTY", "OT_E_INVAL", "OT_E_CLOSED", "OT_E_STATE", "OT_FP32", "OT_BF16",
     "OT_SURROGATE_KEEP_GRADS", "OT_POLICY_RESERVOIR", "OT_POLICY_FIFO", "OT_POLICY_FIRO",
 ]
@@ -309,6 +312,224 @@ class Surrogate:
             pass
 
 
+def _matrix(t, rows: int, cols: int, dtype, what: str):
+    """(pointer, leading dimension) of a rows x cols device tensor with unit column stride."""
+    if t.dtype != dtype or tuple(t.shape) != (rows, cols) or (rows > 0 and cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected a {rows} x {cols} {dtype} tensor with unit column stride")
+    return _dev_ptr(t), t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _bank(t, n: int, rank: int, cols: int, dtype, what: str):
+    """(pointer, leading dimension) of an n x rank x cols device tensor whose rows follow each other."""
+    if t.dtype != dtype or tuple(t.shape) != (n, rank, cols) or (cols > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what}: expected a {n} x {rank} x {cols} {dtype} tensor with unit column stride")
+    ld = t.stride(1) if rank > 1 else t.stride(0) if n > 1 else max(t.stride(0), cols)
+    if n > 1 and t.stride(0) != rank * ld:
+        raise ValueError(f"{what}: the rows of successive adapters must follow each other")
+    return _dev_ptr(t), ld
+
+
+def _vector(t, n: int, dtype, what: str):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {n} values")
+    return _dev_ptr(t)
+
+
+class LowRankAdapters:
+    """Sizes and workspaces of a bank of low-rank adapters beside one frozen layer
+    (include/adapters.h).  Tensors: x (n, in), w (out, in), down (G, rank, in), up
+    (G, rank, out), ids int32 (n), bias fp32 (out), scale fp32 (G), t fp32 (n, rank)."""
+
+    def __init__(self, in_dim: int, out_dim: int, rank: int, n_adapters: int, precision: int = OT_FP32,
+                 max_rows: int = 1024):
+        import torch
+        h = C.c_void_p()
+        check("adapters_create", load().adapters_create(C.byref(h), in_dim, out_dim, rank, n_adapters, precision,
+                                                        max_rows))
+        self._h = h
+        self.in_dim, self.out_dim, self.rank, self.n_adapters = in_dim, out_dim, rank, n_adapters
+        self.precision = precision
+        self.dtype = torch.bfloat16 if precision == OT_BF16 else torch.float32
+
+    @property
+    def handle(self):
+        return self._h
+
+    def _common(self, x, down, up, ids, scale):
+        import torch
+        n = x.shape[0]
+        g, r = self.n_adapters, self.rank
+        return (n, _matrix(x, n, self.in_dim, self.dtype, "x"),
+                (None, 0) if down is None else _bank(down, g, r, self.in_dim, self.dtype, "down"),
+                _bank(up, g, r, self.out_dim, self.dtype, "up"),
+                _vector(ids, n, torch.int32, "ids"), _vector(scale, g, torch.float32, "scale"))
+
+    def forward(self, x, w, down, up, ids, y, bias=None, scale=None, t=None, relu: bool = False, stream=None) -> None:
+        """y = x W^T + bias + scale (x down^T) up per row's adapter (ids), in y's type
+        (float32 or bfloat16); t receives x down^T for backward()."""
+        import torch
+        n, xp, dp, up_, ip, sp = self._common(x, down, up, ids, scale)
+        wp = _matrix(w, self.out_dim, self.in_dim, self.dtype, "w")
+        if y.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("y: expected float32 or bfloat16")
+        yp = _matrix(y, n, self.out_dim, y.dtype, "y")
+        tp = (None, 0) if t is None else _matrix(t, n, self.rank, torch.float32, "t")
+        check("adapters_forward", load().adapters_forward(
+            self._h, *xp, *wp, _vector(bias, self.out_dim, torch.float32, "bias"), *dp, *up_, sp, ip, n, *yp,
+            OT_BF16 if y.dtype == torch.bfloat16 else OT_FP32, *tp, OT_ADAPTERS_RELU if relu else 0,
+            _stream_handle(stream)))
+
+    def backward(self, x, w, down, up, ids, dy, t, ddown, dup, dx=None, scale=None, relu_input: bool = False,
+                 stream=None) -> None:
+        """Gradients of the bank into ddown, dup (fp32, whole) and, if given, of x into dx
+        (relu_input: zero where x is not above 0); w and down may be None without dx."""
+        import torch
+        n, xp, dp, up_, ip, sp = self._common(x, down, up, ids, scale)
+        g, r = self.n_adapters, self.rank
+        if dx is not None and (w is None or down is None):
+            raise ValueError("dx needs w and down")
+        wp = (None, 0) if w is None else _matrix(w, self.out_dim, self.in_dim, self.dtype, "w")
+        dyp = _matrix(dy, n, self.out_dim, self.dtype, "dy")
+        tp = _matrix(t, n, r, torch.float32, "t")
+        ddp = _bank(ddown, g, r, self.in_dim, torch.float32, "ddown")
+        dup_ = _bank(dup, g, r, self.out_dim, torch.float32, "dup")
+        dxp = (None, 0) if dx is None else _matrix(dx, n, self.in_dim, self.dtype, "dx")
+        check("adapters_backward", load().adapters_backward(
+            self._h, *xp, *wp, *dp, *up_, sp, ip, n, *dyp, *tp, *ddp, *dup_, *dxp,
+            OT_ADAPTERS_RELU_INPUT if relu_input else 0, _stream_handle(stream)))
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            check("adapters_destroy", load().adapters_destroy(self._h))
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _list_arrays(tensors, dtypes, counts, what: str):
+    """Host array of the device addresses of a list of contiguous tensors (None: NULL entries allowed)."""
+    if len(tensors) != len(counts):
+        raise ValueError(f"{what}: expected {len(counts)} tensors")
+    out = (C.c_void_p * len(counts))()
+    for i, (t, n) in enumerate(zip(tensors, counts)):
+        if t is None:
+            continue
+        if t.dtype != dtypes[i] or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{what}[{i}]: expected a contiguous {dtypes[i]} tensor of {n} elements")
+        out[i] = _dev_ptr(t) if n else None
+    return out
+
+
+class GradientClip:
+    """A list of gradient tensors (contiguous, float32 or bfloat16) clipped by their
+    global norm, in place or into the tensors `out` (include/gradients.h).  The object
+    keeps the tensors."""
+
+    def __init__(self, grads, out=None):
+        import torch
+        self.grads = list(grads)
+        self.out = None if out is None else list(out)
+        n = len(self.grads)
+        counts = (C.c_int64 * n)(*[t.numel() for t in self.grads])
+        types = (C.c_int32 * n)()
+        for i, t in enumerate(self.grads):
+            if t.dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError(f"grads[{i}]: expected float32 or bfloat16")
+            types[i] = OT_BF16 if t.dtype == torch.bfloat16 else OT_FP32
+        dtypes = [t.dtype for t in self.grads]
+        g = _list_arrays(self.grads, dtypes, counts, "grads")
+        o = None if self.out is None else _list_arrays(self.out, dtypes, counts, "out")
+        h = C.c_void_p()
+        check("clip_create", load().clip_create(C.byref(h), n, g, o, counts, types))
+        self._h = h
+
+    def norm(self, norm, stream=None) -> None:
+        """The global norm into the device scalar `norm`."""
+        check("clip_norm", load().clip_norm(self._h, _scalar(norm, "norm"), _stream_handle(stream)))
+
+    def apply(self, max_norm: float, norm=None, stream=None) -> None:
+        """Scale every tensor by min(1, max_norm / norm); the norm into `norm` (nullable)."""
+        check("clip_apply", load().clip_apply(self._h, max_norm, _scalar(norm, "norm"), _stream_handle(stream)))
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            check("clip_destroy", load().clip_destroy(self._h))
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _scalar(t, what: str):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != 1:
+        raise ValueError(f"{what}: expected a float32 tensor of one element")
+    return _dev_ptr(t)
+
+
+class AdamTensors:
+    """Adam over lists of contiguous fp32 tensors with their gradients clipped by the
+    global norm (include/gradients.h); copies: bf16 tensors (or None) refreshed by
+    each step.  The object keeps the tensors."""
+
+    def __init__(self, params, grads, m, v, copies=None, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+                 eps: float = 1e-8, steps: int = 0):
+        import torch
+        self.params, self.grads, self.m, self.v = list(params), list(grads), list(m), list(v)
+        self.copies = None if copies is None else list(copies)
+        n = len(self.params)
+        counts = (C.c_int64 * n)(*[t.numel() for t in self.params])
+        f32 = [torch.float32] * n
+        arrays = []
+        for name in ("params", "grads", "m", "v"):
+            tensors = getattr(self, name)
+            if any(t is None for t in tensors):
+                raise ValueError(f"{name}: None among the tensors")
+            arrays.append(_list_arrays(tensors, f32, counts, name))
+        c = None if self.copies is None else _list_arrays(self.copies, [torch.bfloat16] * n, counts, "copies")
+        h = C.c_void_p()
+        check("adam_create", load().adam_create(C.byref(h), n, *arrays, c, counts, lr, beta1, beta2, eps, steps))
+        self._h = h
+
+    def step(self, max_norm: float = 0.0, norm=None, stream=None) -> None:
+        """One step; max_norm 0: gradients as they are.  norm (nullable): the norm before
+        clipping.  A norm that is not finite takes no step."""
+        check("adam_step", load().adam_step(self._h, max_norm, _scalar(norm, "norm"), _stream_handle(stream)))
+
+    def set_lr(self, lr: float) -> None:
+        check("adam_set_lr", load().adam_set_lr(self._h, lr))
+
+    def get_steps(self) -> int:
+        n = C.c_int64()
+        check("adam_get_steps", load().adam_get_steps(self._h, C.byref(n)))
+        return n.value
+
+    def set_steps(self, steps: int) -> None:
+        check("adam_set_steps", load().adam_set_steps(self._h, steps))
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            check("adam_destroy", load().adam_destroy(self._h))
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 # ---- C-named entry points (argument marshalling only) ----------------------------
 def reservoir_create(capacity, threshold, x_dim, u_dim, seed, policy=OT_POLICY_RESERVOIR,
                      order_stream=None) -> Reservoir:
@@ -402,3 +623,62 @@ def surrogate_predict_noalloc(s: Surrogate, x, y, stream=None) -> None:
 
 def surrogate_destroy(s: Surrogate) -> None:
     s.close()
+
+
+def adapters_create(in_dim, out_dim, rank, n_adapters, precision=OT_FP32, max_rows=1024) -> LowRankAdapters:
+    return LowRankAdapters(in_dim, out_dim, rank, n_adapters, precision, max_rows)
+
+
+def adapters_forward(a: LowRankAdapters, x, w, down, up, ids, y, bias=None, scale=None, t=None, relu=False,
+                     stream=None) -> None:
+    a.forward(x, w, down, up, ids, y, bias, scale, t, relu, stream)
+
+
+def adapters_backward(a: LowRankAdapters, x, w, down, up, ids, dy, t, ddown, dup, dx=None, scale=None,
+                      relu_input=False, stream=None) -> None:
+    a.backward(x, w, down, up, ids, dy, t, ddown, dup, dx, scale, relu_input, stream)
+
+
+def adapters_destroy(a: LowRankAdapters) -> None:
+    a.close()
+
+
+def clip_create(grads, out=None) -> GradientClip:
+    return GradientClip(grads, out)
+
+
+def clip_norm(c: GradientClip, norm, stream=None) -> None:
+    c.norm(norm, stream)
+
+
+def clip_apply(c: GradientClip, max_norm, norm=None, stream=None) -> None:
+    c.apply(max_norm, norm, stream)
+
+
+def clip_destroy(c: GradientClip) -> None:
+    c.close()
+
+
+def adam_create(params, grads, m, v, copies=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
+                steps=0) -> AdamTensors:
+    return AdamTensors(params, grads, m, v, copies, lr, beta1, beta2, eps, steps)
+
+
+def adam_step(a: AdamTensors, max_norm=0.0, norm=None, stream=None) -> None:
+    a.step(max_norm, norm, stream)
+
+
+def adam_set_lr(a: AdamTensors, lr) -> None:
+    a.set_lr(lr)
+
+
+def adam_get_steps(a: AdamTensors) -> int:
+    return a.get_steps()
+
+
+def adam_set_steps(a: AdamTensors, steps) -> None:
+    a.set_steps(steps)
+
+
+def adam_destroy(a: AdamTensors) -> None:
+    a.close()

@@ -1,4 +1,5 @@
-"""ctypes declarations of the C ABI (include/ot_status.h, reservoir.h, surrogate.h).
+"""ctypes declarations of the C ABI (include/ot_status.h, reservoir.h, surrogate.h, adapters.h,
+gradients.h).
 
 Argument marshalling only.  Loading fails loudly when the library has not been
 built: there is no fallback implementation.
@@ -22,6 +23,8 @@ OT_E_STATE = -5
 OT_FP32 = 0
 OT_BF16 = 1
 OT_SURROGATE_KEEP_GRADS = 1
+OT_ADAPTERS_RELU = 1
+OT_ADAPTERS_RELU_INPUT = 2
 OT_POLICY_RESERVOIR = 0
 OT_POLICY_FIFO = 1
 OT_POLICY_FIRO = 2
@@ -81,6 +84,22 @@ SIGNATURES = {
     "surrogate_timing_begin": (C.c_int, [vp, u32, i64]),
     "surrogate_timing_end": (C.c_int, [vp, vp, vp]),
     "surrogate_destroy": (C.c_int, [vp]),
+    "adapters_create": (C.c_int, [C.POINTER(vp), i64, i64, i32, i32, i32, i64]),
+    "adapters_forward": (C.c_int, [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, i32, vp, i64,
+                                   u32, vp]),
+    "adapters_backward": (C.c_int, [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, i64,
+                                    vp, i64, vp, i64, u32, vp]),
+    "adapters_destroy": (C.c_int, [vp]),
+    "clip_create": (C.c_int, [C.POINTER(vp), i32, vp, vp, vp, vp]),
+    "clip_norm": (C.c_int, [vp, vp, vp]),
+    "clip_apply": (C.c_int, [vp, f32, vp, vp]),
+    "clip_destroy": (C.c_int, [vp]),
+    "adam_create": (C.c_int, [C.POINTER(vp), i32, vp, vp, vp, vp, vp, vp, f32, f32, f32, f32, i64]),
+    "adam_step": (C.c_int, [vp, f32, vp, vp]),
+    "adam_set_lr": (C.c_int, [vp, f32]),
+    "adam_get_steps": (C.c_int, [vp, C.POINTER(i64)]),
+    "adam_set_steps": (C.c_int, [vp, i64]),
+    "adam_destroy": (C.c_int, [vp]),
 }
 
 _lib = None
