@@ -12,22 +12,10 @@
 #include "adapters.h"
 #include "common.h"
 #include "intmath.h"
+#include "lowrank.h"
 #include "surrogate.h"
 
 namespace ot {
-
-constexpr int kSlotRows = 32;       // sorted rows of one adapter that a block takes together
-
-// Rows [start, start + count) of the sorted order, all of adapter g.
-struct RowSlot {
-  int32_t start, count, g, pad;
-};
-
-__device__ __forceinline__ float lr_value(const float* p) { return *p; }
-__device__ __forceinline__ float lr_value(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ __forceinline__ void lr_store(float* p, float v) { *p = v; }
-// round to nearest even, NaN stays NaN
-__device__ __forceinline__ void lr_store(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
 
 // Block g collects the rows of adapter g (block G: rows without one) in their
 // order: it counts the rows of smaller keys, which is where its own start, and
@@ -86,44 +74,6 @@ __global__ __launch_bounds__(256) void group_rows_kernel(const int32_t* __restri
       gid[p] = g;
     }
     at += (s_same[0] + s_same[1]) + (s_same[2] + s_same[3]);
-  }
-}
-
-struct ShrinkArgs {
-  const void* src;        // rows of L values
-  int64_t lds;
-  const void* mat;        // G x R rows of L values
-  int64_t ldm;
-  int64_t L;
-  int32_t G, R, RP;
-  const float* scale;     // nullable
-  const int32_t* perm;
-  const RowSlot* slots;
-  float* ts;              // sorted, pitch RP: scaled
-  float* t;               // by row, pitch ldt: unscaled (nullable)
-  int64_t ldt;
-};
-
-// t = mat_g src of every row of a slot.
-template <class T>
-__global__ __launch_bounds__(256) void shrink_kernel(ShrinkArgs a) {
-  const RowSlot s = a.slots[blockIdx.x];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  for (int i = wid; i < s.count; i += 4) {
-    const int64_t row = a.perm[s.start + i];
-    const T* x = static_cast<const T*>(a.src) + row * a.lds;
-    for (int r = 0; r < a.RP; ++r) {
-      float v = 0.f;
-      if (s.g < a.G && r < a.R) {
-        const T* q = static_cast<const T*>(a.mat) + ((int64_t)s.g * a.R + r) * a.ldm;
-        for (int64_t k = lane; k < a.L; k += 64) v = fmaf(lr_value(x + k), lr_value(q + k), v);
-        v = warp_sum(v);
-      }
-      if (lane == 0) {
-        if (a.t && r < a.R) a.t[row * a.ldt + r] = v;
-        if (s.g < a.G) a.ts[(int64_t)(s.start + i) * a.RP + r] = a.scale ? a.scale[s.g] * v : v;
-      }
-    }
   }
 }
 
@@ -194,39 +144,6 @@ __global__ __launch_bounds__(256) void expand_kernel(ExpandArgs a) {
   }
 }
 
-struct OuterArgs {
-  const void* src;        // rows of L values
-  int64_t lds;
-  int64_t L;
-  const float* coef;      // sorted rows (pitch RP) or, by_row, the caller's rows (pitch ldc)
-  int64_t ldc;
-  int32_t by_row;
-  const float* scale;     // by_row: factor of adapter g (nullable)
-  int32_t R;
-  const int32_t* perm;
-  const int32_t* off;
-  float* out;             // G x R rows of L values
-  int64_t ldo;
-};
-
-// out_g[r][c] = sum over the adapter's rows of coef[row][r] src[row][c].
-template <class T>
-__global__ __launch_bounds__(256) void outer_kernel(OuterArgs a) {
-  const int g = blockIdx.y;
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.L) return;
-  const int b = a.off[g], e = a.off[g + 1];
-  const float sc = a.by_row && a.scale ? a.scale[g] : 1.f;
-  for (int r = 0; r < a.R; ++r) {
-    float v = 0.f;
-    for (int p = b; p < e; ++p) {
-      const int64_t row = a.perm[p];
-      v = fmaf(a.coef[(a.by_row ? row : p) * a.ldc + r], lr_value(static_cast<const T*>(a.src) + row * a.lds + c), v);
-    }
-    a.out[((int64_t)g * a.R + r) * a.ldo + c] = sc * v;
-  }
-}
-
 }  // namespace ot
 
 struct ot_adapters {
@@ -244,12 +161,25 @@ namespace {
 
 constexpr int64_t kMaxRows = 1LL << 20;
 
+// Splits of the shrink's k range (length L) for n rows: enough blocks to fill the
+// card, each with at least 16 steps per wavefront; one when the range is short,
+// since the join costs a launch.  Blocks of unused slots (a large bank, few rows) are
+// not multiplied without bound.
+constexpr int64_t kShrinkBlocks = 1024;
+int64_t shrink_splits(int64_t n, int64_t L, int32_t G) {
+  if (L <= 4096) return 1;
+  const int64_t slots = ot::ceil_div(n, ot::kSlotRows) + std::min<int64_t>(G, n) / 2;
+  return std::max<int64_t>(1, std::min(std::min(ot::ceil_div(kShrinkBlocks, slots), L / 2048),
+                                       32768 / (n / ot::kSlotRows + G + 1)));
+}
+
 struct Work {
   int32_t* perm;
   int32_t* gid;
   int32_t* off;
   ot::RowSlot* slots;
   float* ts;
+  float* part;
   int64_t n_slots;
 };
 
@@ -270,6 +200,9 @@ int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
   t.off = reinterpret_cast<int32_t*>(take(4 * (a->G + 2)));
   t.slots = reinterpret_cast<ot::RowSlot*>(take((int64_t)sizeof(ot::RowSlot) * t.n_slots));
   t.ts = reinterpret_cast<float*>(take(4 * n * a->RP));
+  // splits * rows of any call of up to n rows: splits <= kShrinkBlocks / (rows / 32) + 1
+  const bool split = std::max(a->in, a->out) > 4096;
+  t.part = reinterpret_cast<float*>(take(split ? 4 * (kShrinkBlocks * ot::kSlotRows + n) * a->RP : 0));
   if (w) *w = t;
   return at;
 }
@@ -331,9 +264,24 @@ int check_values(const void* p, int align, const char* what, const char* name) {
 }
 
 template <class T>
-int run_shrink(const ot::ShrinkArgs& s, int64_t n_slots, hipStream_t st) {
-  hipLaunchKernelGGL(ot::shrink_kernel<T>, dim3((unsigned)n_slots), dim3(256), 0, st, s);
+int run_shrink(ot::ShrinkArgs s, int64_t n, const Work& w, hipStream_t st) {
+  const int64_t splits = shrink_splits(n, s.L, s.G);
+  s.k_chunk = ot::ceil_div(ot::ceil_div(s.L, splits), ot::kShrinkUnit) * ot::kShrinkUnit;
+  s.splits = (int32_t)ot::ceil_div(s.L, s.k_chunk);
+  s.n = n;
+  s.part = w.part;
+  const dim3 grid((unsigned)w.n_slots, (unsigned)s.splits);
+  switch (s.RP / 16) {
+    case 1: hipLaunchKernelGGL((ot::shrink_kernel<T, 1>), grid, dim3(256), 0, st, s); break;
+    case 2: hipLaunchKernelGGL((ot::shrink_kernel<T, 2>), grid, dim3(256), 0, st, s); break;
+    case 3: hipLaunchKernelGGL((ot::shrink_kernel<T, 3>), grid, dim3(256), 0, st, s); break;
+    default: hipLaunchKernelGGL((ot::shrink_kernel<T, 4>), grid, dim3(256), 0, st, s); break;
+  }
   OT_LAUNCHED("shrink_kernel");
+  if (s.splits > 1) {
+    hipLaunchKernelGGL(ot::shrink_reduce_kernel, dim3((unsigned)w.n_slots), dim3(256), 0, st, s);
+    OT_LAUNCHED("shrink_reduce_kernel");
+  }
   return OT_OK;
 }
 
@@ -345,11 +293,28 @@ int run_expand(const ot::ExpandArgs& e, hipStream_t st) {
   return OT_OK;
 }
 
-template <class T>
-int run_outer(const ot::OuterArgs& o, int32_t G, hipStream_t st) {
-  hipLaunchKernelGGL(ot::outer_kernel<T>, dim3((unsigned)ot::ceil_div(o.L, 256), (unsigned)G), dim3(256), 0, st, o);
+template <class T, int NT>
+int launch_outer(const ot::OuterArgs& o, int32_t G, hipStream_t st) {
+  // short rows: the wavefronts of a block share its columns and split the rows
+  const int64_t blocks = ot::ceil_div(o.L, 256) * G;
+  if (blocks < 1024)
+    hipLaunchKernelGGL((ot::outer_kernel<T, NT, true>), dim3((unsigned)ot::ceil_div(o.L, 64), (unsigned)G), dim3(256),
+                       0, st, o);
+  else
+    hipLaunchKernelGGL((ot::outer_kernel<T, NT, false>), dim3((unsigned)ot::ceil_div(o.L, 256), (unsigned)G), dim3(256),
+                       0, st, o);
   OT_LAUNCHED("outer_kernel");
   return OT_OK;
+}
+
+template <class T>
+int run_outer(const ot::OuterArgs& o, int32_t G, hipStream_t st) {
+  switch ((o.R + 15) / 16) {
+    case 1: return launch_outer<T, 1>(o, G, st);
+    case 2: return launch_outer<T, 2>(o, G, st);
+    case 3: return launch_outer<T, 3>(o, G, st);
+    default: return launch_outer<T, 4>(o, G, st);
+  }
 }
 
 int run_group(const ot_adapters* a, const int32_t* ids, int64_t n, const Work& w, hipStream_t st) {
@@ -422,8 +387,9 @@ extern "C" int adapters_forward(ot_adapters* a, const void* x, int64_t ldx, cons
   Work wk;
   layout(a, n, a->ws, &wk);
   if ((rc = run_group(a, ids, n, wk, st))) return rc;
-  const ot::ShrinkArgs s{x, ldx, down, ldd, a->in, a->G, a->R, a->RP, scale, wk.perm, wk.slots, wk.ts, t, ldt};
-  rc = e == 2 ? run_shrink<uint16_t>(s, wk.n_slots, st) : run_shrink<float>(s, wk.n_slots, st);
+  const ot::ShrinkArgs s{x,     ldx,     down,     ldd,     a->in, 0, a->G, a->R, a->RP, 0, 0,
+                         scale, wk.perm, wk.slots, nullptr, wk.ts, t, ldt};
+  rc = e == 2 ? run_shrink<uint16_t>(s, n, wk, st) : run_shrink<float>(s, n, wk, st);
   if (rc) return rc;
   const ot::ExpandArgs ex{x,    ldx,     w,       ldw,  n,  a->out, a->in, wk.ts, up, ldu, a->G, a->R, a->RP,
                           wk.perm, wk.gid, bias, (int32_t)(flags & OT_ADAPTERS_RELU ? 1 : 0), nullptr, 0, y, ldy};
@@ -471,9 +437,9 @@ extern "C" int adapters_backward(ot_adapters* a, const void* x, int64_t ldx, con
   layout(a, n, a->ws, &wk);
   if ((rc = run_group(a, ids, n, wk, st))) return rc;
   if (n > 0) {
-    const ot::ShrinkArgs s{dy,      lddy,     up,    ldu,     a->out, a->G, a->R, a->RP, scale,
-                           wk.perm, wk.slots, wk.ts, nullptr, 0};
-    rc = e == 2 ? run_shrink<uint16_t>(s, wk.n_slots, st) : run_shrink<float>(s, wk.n_slots, st);
+    const ot::ShrinkArgs s{dy,    lddy,    up,       ldu,     a->out, 0, a->G, a->R, a->RP, 0, 0,
+                           scale, wk.perm, wk.slots, nullptr, wk.ts, nullptr, 0};
+    rc = e == 2 ? run_shrink<uint16_t>(s, n, wk, st) : run_shrink<float>(s, n, wk, st);
     if (rc) return rc;
   }
   const ot::OuterArgs ou{dy, lddy, a->out, t, ldt, 1, scale, a->R, wk.perm, wk.off, dup, lddu};
