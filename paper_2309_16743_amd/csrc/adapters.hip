@@ -11,6 +11,8 @@
 
 #include "adapters.h"
 #include "common.h"
+#include "gemm_bf16.h"
+#include "gemm_f32x3.h"
 #include "intmath.h"
 #include "lowrank.h"
 #include "surrogate.h"
@@ -77,70 +79,33 @@ __global__ __launch_bounds__(256) void group_rows_kernel(const int32_t* __restri
   }
 }
 
-struct ExpandArgs {
-  const void* A;          // rows (through perm) of K values
-  int64_t lda;
-  const void* B;          // KMajor: N rows of K values; else K rows of N values
-  int64_t ldb;
-  int64_t M, N, K;
-  const float* ts;        // sorted low-rank values, pitch RP
-  const void* L;          // G x R rows of N values
-  int64_t ldl;
-  int32_t G, R, RP;
-  const int32_t* perm;
-  const int32_t* gid;
-  const float* bias;      // nullable
-  int32_t relu;
-  const void* mask;       // rows by row number; the output is 0 where it is not above 0 (nullable)
-  int64_t ldmask;
-  void* C;
-  int64_t ldc;
-};
-
-// C[row] = B A[row] (+ bias) + sum_r ts[r] L_g[r], 64 x 64 per block.
-template <class T, class TC, bool KMAJOR>
-__global__ __launch_bounds__(256) void expand_kernel(ExpandArgs a) {
-  __shared__ float sa[16][65], sb[16][65];
-  const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-  const int64_t tiles_m = (a.M + 63) / 64;
-  const int64_t m0 = (blockIdx.x % tiles_m) * 64, n0 = (blockIdx.x / tiles_m) * 64;
-  const T* A = static_cast<const T*>(a.A);
-  const T* B = static_cast<const T*>(a.B);
-  float acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < a.K; k0 += 16) {
-    for (int i = tid; i < 1024; i += 256) {
-      const int r = i / 16, k = i % 16;
-      sa[k][r] = (m0 + r < a.M && k0 + k < a.K) ? lr_value(A + a.perm[m0 + r] * a.lda + k0 + k) : 0.f;
-      if (KMAJOR) {
-        sb[k][r] = (n0 + r < a.N && k0 + k < a.K) ? lr_value(B + (n0 + r) * a.ldb + k0 + k) : 0.f;
-      } else {
-        const int kk = i / 64, c = i % 64;
-        sb[kk][c] = (n0 + c < a.N && k0 + kk < a.K) ? lr_value(B + (k0 + kk) * a.ldb + n0 + c) : 0.f;
-      }
-    }
-    __syncthreads();
-    for (int k = 0; k < 16; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][4 * ty + i], sb[k][tx + 16 * j], acc[i][j]);
-    __syncthreads();
+// C[row of m][n] = sum of the splits' partials [split][m][n] in order, 0 where mask is not above 0; four columns
+// per thread.
+template <class T>
+__global__ __launch_bounds__(256) void adapt_reduce_kernel(const float* __restrict__ ws, int32_t splits,
+                                                           int64_t stride, int64_t M, int64_t N, int64_t ldws,
+                                                           const int32_t* __restrict__ perm,
+                                                           const T* __restrict__ mask, int64_t ldmask,
+                                                           T* __restrict__ C, int64_t ldc) {
+  const int64_t groups = (N + 3) / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= M * groups) return;
+  const int64_t m = i / groups, n = i % groups * 4, row = perm[m];
+  const float* p = ws + m * ldws + n;
+  f32x4 v = *reinterpret_cast<const f32x4*>(p);
+  int s = 1;
+  for (; s + 8 <= splits; s += 8) {                    // eight loads in flight, added in order
+    f32x4 t[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) t[u] = *reinterpret_cast<const f32x4*>(p + (s + u) * stride);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += t[u];
   }
-  for (int i = 0; i < 4; ++i) {
-    const int64_t p = m0 + 4 * ty + i;
-    if (p >= a.M) continue;
-    const int64_t row = a.perm[p];
-    const int g = a.gid[p];
-    for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + tx + 16 * j;
-      if (n >= a.N) continue;
-      float v = acc[i][j];
-      if (g < a.G)
-        for (int r = 0; r < a.R; ++r)
-          v = fmaf(a.ts[p * a.RP + r], lr_value(static_cast<const T*>(a.L) + ((int64_t)g * a.R + r) * a.ldl + n), v);
-      if (a.bias) v += a.bias[n];
-      if (a.relu) v = v > 0.f ? v : (v != v ? v : 0.f);
-      if (a.mask && !(lr_value(static_cast<const T*>(a.mask) + row * a.ldmask + n) > 0.f)) v = 0.f;
-      lr_store(static_cast<TC*>(a.C) + row * a.ldc + n, v);
-    }
+  for (; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * stride);
+  const int cnt = (int)min((int64_t)4, N - n);
+  for (int c = 0; c < cnt; ++c) {
+    if (mask && !(lr_value(mask + row * ldmask + n + c) > 0.f)) v[c] = 0.f;
+    lr_store(C + row * ldc + n + c, v[c]);
   }
 }
 
@@ -173,17 +138,84 @@ int64_t shrink_splits(int64_t n, int64_t L, int32_t G) {
                                        32768 / (n / ot::kSlotRows + G + 1)));
 }
 
+// Block tiles (rows x columns): of gemm_bf16.h, then of gemm_f32x3.h.
+enum Tile : int {
+  kB64x64, kB64x128, kB128x128, kB128x256, kB256x256,
+  kX128x128, kX64x64, kX64x128, kX32x256, kX64x256
+};
+constexpr int kTileRows[] = {64, 64, 128, 128, 256, 128, 64, 64, 32, 64};
+constexpr int kTileCols[] = {64, 128, 128, 256, 256, 128, 64, 128, 256, 256};
+
+struct Plan {
+  int tile;
+  int64_t splits, k_chunk;
+};
+
+int64_t tiles_of(int tile, int64_t M, int64_t N) {
+  return ot::ceil_div(M, kTileRows[tile]) * ot::ceil_div(N, kTileCols[tile]);
+}
+
+// `want` splits of K, in k tiles of 64, as many as are not empty.
+Plan split_plan(int tile, int64_t K, int64_t want) {
+  Plan p{tile, 1, K};
+  if (want > 1) {
+    p.k_chunk = ot::ceil_div(ot::ceil_div(K, want), 64) * 64;
+    p.splits = ot::ceil_div(K, p.k_chunk);
+    if (p.splits == 1) p.k_chunk = K;
+  }
+  return p;
+}
+
+Plan plan_expand(bool bf16, bool kmajor, int64_t M, int64_t N, int64_t K) {
+  constexpr int64_t kCUs = 256;
+  if (bf16) {
+    if (kmajor) {
+      if (M > 128 && tiles_of(kB256x256, M, N) >= kCUs - 16) return split_plan(kB256x256, K, 1);
+      if (M > 64 && tiles_of(kB128x256, M, N) >= kCUs - 16) return split_plan(kB128x256, K, 1);
+      if (M <= 64 && tiles_of(kB64x128, M, N) >= kCUs - 16) return split_plan(kB64x128, K, 1);
+      if (tiles_of(kB128x128, M, N) >= 2 * kCUs - 32) return split_plan(kB128x128, K, 1);
+      if (tiles_of(kB64x128, M, N) >= 2 * kCUs - 32) return split_plan(kB64x128, K, 1);
+      return split_plan(kB64x64, K, 1);
+    }
+    const int big = M > 128 ? kB256x256 : M > 64 ? kB128x256 : kB64x128;
+    const int64_t t = tiles_of(big, M, N), sp = ot::ceil_div(kCUs - 16, t);
+    if (K / sp >= 2048) return split_plan(big, K, sp);
+    const int64_t t2 = tiles_of(kB64x128, M, N);
+    return split_plan(kB64x128, K, std::max<int64_t>(1, std::min(ot::ceil_div(kCUs - 16, t2), K / 512)));
+  }
+  if (kmajor) {
+    if (M <= 32 && tiles_of(kX32x256, M, N) >= kCUs) return split_plan(kX32x256, K, 1);
+    if (M <= 64 && tiles_of(kX64x256, M, N) >= kCUs) return split_plan(kX64x256, K, 1);
+    return split_plan(tiles_of(kX64x128, M, N) >= 2 * kCUs ? kX64x128 : kX64x64, K, 1);
+  }
+  const int tile = M <= 32 && N > 128 ? kX32x256 : M <= 64 && N > 128 ? kX64x256 : M <= 64 || N <= 64 ? kX64x64 : kX128x128;
+  return split_plan(tile, K, std::max<int64_t>(1, std::min(2 * kCUs / tiles_of(tile, M, N), K / 128)));
+}
+
+// Partial sums of the plan (fp32 values; 0: not split).
+int64_t plan_values(const Plan& p, int64_t M, int64_t N) { return p.splits > 1 ? p.splits * M * ((N + 3) / 4 * 4) : 0; }
+
 struct Work {
   int32_t* perm;
   int32_t* gid;
   int32_t* off;
   ot::RowSlot* slots;
   float* ts;
-  float* part;
+  float* part;            // partial sums of split products, one after another
   int64_t n_slots;
 };
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+
+// Partial sums that a call of up to n rows needs.
+int64_t part_values(const ot_adapters* a, int64_t n) {
+  // shrinks: splits * rows, with splits <= kShrinkBlocks / (rows / 32) + 1
+  int64_t most = std::max(a->in, a->out) > 4096 ? (kShrinkBlocks * ot::kSlotRows + n) * a->RP : 0;
+  // the input gradient: a plan depends on the rows only through whole groups of 32
+  for (int64_t m = 32; m < n + 32; m += 32)
+    most = std::max(most, plan_values(plan_expand(a->precision == OT_BF16, false, m, a->in, a->out), m, a->in));
+  return most;
+}
 
 // Workspace of a call of n rows at `base`; returns its size.
 int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
@@ -200,9 +232,7 @@ int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
   t.off = reinterpret_cast<int32_t*>(take(4 * (a->G + 2)));
   t.slots = reinterpret_cast<ot::RowSlot*>(take((int64_t)sizeof(ot::RowSlot) * t.n_slots));
   t.ts = reinterpret_cast<float*>(take(4 * n * a->RP));
-  // splits * rows of any call of up to n rows: splits <= kShrinkBlocks / (rows / 32) + 1
-  const bool split = std::max(a->in, a->out) > 4096;
-  t.part = reinterpret_cast<float*>(take(split ? 4 * (kShrinkBlocks * ot::kSlotRows + n) * a->RP : 0));
+  t.part = reinterpret_cast<float*>(take(4 * part_values(a, n)));
   if (w) *w = t;
   return at;
 }
@@ -285,14 +315,6 @@ int run_shrink(ot::ShrinkArgs s, int64_t n, const Work& w, hipStream_t st) {
   return OT_OK;
 }
 
-template <class T, class TC, bool KMAJOR>
-int run_expand(const ot::ExpandArgs& e, hipStream_t st) {
-  const int64_t tiles = ot::ceil_div(e.M, 64) * ot::ceil_div(e.N, 64);
-  hipLaunchKernelGGL((ot::expand_kernel<T, TC, KMAJOR>), dim3((unsigned)tiles), dim3(256), 0, st, e);
-  OT_LAUNCHED("expand_kernel");
-  return OT_OK;
-}
-
 template <class T, int NT>
 int launch_outer(const ot::OuterArgs& o, int32_t G, hipStream_t st) {
   // short rows: the wavefronts of a block share its columns and split the rows
@@ -315,6 +337,107 @@ int run_outer(const ot::OuterArgs& o, int32_t G, hipStream_t st) {
     case 3: return launch_outer<T, 3>(o, G, st);
     default: return launch_outer<T, 4>(o, G, st);
   }
+}
+
+// The adapted product C[row] = B A[row] (+ bias) + sum_r ts[r] mat_g[r] (ReLU or mask): the
+// layer itself (B = W, KMajor) or its input gradient (B = W, MNMajor).
+struct Expand {
+  const void* A;
+  int64_t lda;
+  const void* B;
+  int64_t ldb;
+  int64_t M, N, K;
+  const float* bias;
+  void* C;
+  int64_t ldc;
+  int32_t c_type;         // OT_FP32 or OT_BF16
+  ot::AdaptRows lr;
+};
+
+template <ot::LayB LB, ot::EpiB E>
+hipError_t launch_b(int tile, const ot::GemmBArgs& g, int64_t splits, hipStream_t st) {
+  constexpr ot::LayB KM = ot::LayB::KMajor;
+  if constexpr (LB == KM) {
+    if (tile == kB64x64) return ot::launch_gemm_bf16_pipe<64, 64, 64, 3, 3, KM, LB, E>(g, splits, st);
+  }
+  if (tile == kB64x128) return ot::launch_gemm_bf16_pipe<64, 128, 64, 3, 2, KM, LB, E>(g, splits, st);
+  if (tile == kB128x128) return ot::launch_gemm_bf16_pipe<128, 128, 32, 4, 2, KM, LB, E>(g, splits, st);
+  if (tile == kB128x256) return ot::launch_gemm_bf16_pipe<128, 256, 32, 3, 2, KM, LB, E>(g, splits, st);
+  return ot::launch_gemm_bf16_pp<4, KM, LB, E>(g, splits, st);
+}
+
+template <ot::Lay LB, ot::Epi E>
+hipError_t launch_x(int tile, const ot::GemmArgs& g, int64_t splits, hipStream_t st) {
+  constexpr ot::Lay KM = ot::Lay::KMajor;
+  if (tile == kX64x64) return ot::launch_gemm_f32x3<2, 2, 1, 1, KM, LB, E>(g, splits, st);
+  if (tile == kX64x128) return ot::launch_gemm_f32x3<2, 2, 1, 2, KM, LB, E>(g, splits, st);
+  if (tile == kX32x256) return ot::launch_gemm_f32x3<1, 4, 1, 2, KM, LB, E>(g, splits, st);
+  if (tile == kX64x256) return ot::launch_gemm_f32x3<1, 4, 2, 2, KM, LB, E>(g, splits, st);
+  return ot::launch_gemm_f32x3<2, 2, 2, 2, KM, LB, E>(g, splits, st);
+}
+
+template <class T, class G>
+int reduce_splits(const Expand& e, const G& g, const Plan& p, const float* part, hipStream_t st) {
+  hipLaunchKernelGGL(ot::adapt_reduce_kernel<T>, dim3((unsigned)ot::ceil_div(e.M * ((e.N + 3) / 4), 256)), dim3(256), 0,
+                     st, part, (int32_t)p.splits, g.split_stride, e.M, e.N, g.ldc, e.lr.perm,
+                     static_cast<const T*>(e.lr.mask), e.lr.ldmask, static_cast<T*>(e.C), e.ldc);
+  OT_LAUNCHED("adapt_reduce_kernel");
+  return OT_OK;
+}
+
+// part: workspace of plan_values() floats.  Split products only as input gradients.
+template <class G>
+void fill_expand(G& g, const Expand& e, const Plan& p, float* part) {
+  g.lda = e.lda;
+  g.ldb = e.ldb;
+  g.ldc = e.ldc;
+  g.M = e.M;
+  g.N = e.N;
+  g.K = e.K;
+  g.bias = e.bias;
+  g.lr = e.lr;
+  g.k_chunk = p.k_chunk;
+  if (p.splits > 1) {
+    g.ldc = (e.N + 3) / 4 * 4;
+    g.split_stride = e.M * g.ldc;
+  }
+}
+
+int run_expand(const Expand& e, bool bf16, bool kmajor, float* part, hipStream_t st) {
+  const Plan p = plan_expand(bf16, kmajor, e.M, e.N, e.K);
+  hipError_t rc;
+  if (bf16) {
+    ot::GemmBArgs g{};
+    fill_expand(g, e, p, part);
+    g.A = static_cast<const uint16_t*>(e.A);
+    g.B = static_cast<const uint16_t*>(e.B);
+    g.C = p.splits > 1 ? part : e.C;
+    if (kmajor)
+      rc = e.c_type == OT_BF16 ? launch_b<ot::LayB::KMajor, ot::EpiB::AdaptBf>(p.tile, g, 1, st)
+                               : launch_b<ot::LayB::KMajor, ot::EpiB::AdaptF32>(p.tile, g, 1, st);
+    else if (p.splits > 1)
+      rc = launch_b<ot::LayB::MNMajor, ot::EpiB::AdaptSplit>(p.tile, g, p.splits, st);
+    else
+      rc = launch_b<ot::LayB::MNMajor, ot::EpiB::AdaptBf>(p.tile, g, 1, st);
+    if (rc == hipSuccess && p.splits > 1) return reduce_splits<uint16_t>(e, g, p, part, st);
+  } else {
+    ot::GemmArgs g{};
+    fill_expand(g, e, p, part);
+    g.A = static_cast<const float*>(e.A);
+    g.B = static_cast<const float*>(e.B);
+    g.C = p.splits > 1 ? part : static_cast<float*>(e.C);
+    if (kmajor)
+      rc = e.c_type == OT_BF16 ? launch_x<ot::Lay::KMajor, ot::Epi::AdaptBf>(p.tile, g, 1, st)
+                               : launch_x<ot::Lay::KMajor, ot::Epi::AdaptF32>(p.tile, g, 1, st);
+    else if (p.splits > 1)
+      rc = launch_x<ot::Lay::MNMajor, ot::Epi::AdaptSplit>(p.tile, g, p.splits, st);
+    else
+      rc = launch_x<ot::Lay::MNMajor, ot::Epi::AdaptF32>(p.tile, g, 1, st);
+    if (rc == hipSuccess && p.splits > 1) return reduce_splits<float>(e, g, p, part, st);
+  }
+  if (rc != hipSuccess)
+    return ot::set_error(OT_E_HIP, "launch of the adapted product failed: %s", hipGetErrorString(rc));
+  return OT_OK;
 }
 
 int run_group(const ot_adapters* a, const int32_t* ids, int64_t n, const Work& w, hipStream_t st) {
@@ -391,11 +514,9 @@ extern "C" int adapters_forward(ot_adapters* a, const void* x, int64_t ldx, cons
                          scale, wk.perm, wk.slots, nullptr, wk.ts, t, ldt};
   rc = e == 2 ? run_shrink<uint16_t>(s, n, wk, st) : run_shrink<float>(s, n, wk, st);
   if (rc) return rc;
-  const ot::ExpandArgs ex{x,    ldx,     w,       ldw,  n,  a->out, a->in, wk.ts, up, ldu, a->G, a->R, a->RP,
-                          wk.perm, wk.gid, bias, (int32_t)(flags & OT_ADAPTERS_RELU ? 1 : 0), nullptr, 0, y, ldy};
-  if (e == 2)
-    return y_type == OT_BF16 ? run_expand<uint16_t, uint16_t, true>(ex, st) : run_expand<uint16_t, float, true>(ex, st);
-  return y_type == OT_BF16 ? run_expand<float, uint16_t, true>(ex, st) : run_expand<float, float, true>(ex, st);
+  const ot::AdaptRows lr{wk.perm, wk.gid, wk.off, wk.ts, up, ldu, a->G, a->R, a->RP,
+                         (int32_t)(flags & OT_ADAPTERS_RELU ? 1 : 0), nullptr, 0};
+  return run_expand(Expand{x, ldx, w, ldw, n, a->out, a->in, bias, y, ldy, y_type, lr}, e == 2, true, wk.part, st);
 } catch (const std::bad_alloc&) {
   return ot::set_error(OT_E_NOMEM, "adapters_forward: out of host memory");
 }
@@ -447,12 +568,10 @@ extern "C" int adapters_backward(ot_adapters* a, const void* x, int64_t ldx, con
   if ((rc = e == 2 ? run_outer<uint16_t>(ou, a->G, st) : run_outer<float>(ou, a->G, st))) return rc;
   if ((rc = e == 2 ? run_outer<uint16_t>(od, a->G, st) : run_outer<float>(od, a->G, st))) return rc;
   if (n == 0 || !dx) return OT_OK;
-  const ot::ExpandArgs ex{dy,      lddy,   w,       ldw, n,
-                          a->in,   a->out, wk.ts,   down, ldd,
-                          a->G,    a->R,   a->RP,   wk.perm, wk.gid,
-                          nullptr, 0,      flags & OT_ADAPTERS_RELU_INPUT ? x : nullptr, ldx, dx,
-                          lddx};
-  return e == 2 ? run_expand<uint16_t, uint16_t, false>(ex, st) : run_expand<float, float, false>(ex, st);
+  const ot::AdaptRows lr{wk.perm, wk.gid, wk.off, wk.ts, down, ldd, a->G, a->R, a->RP, 0,
+                         flags & OT_ADAPTERS_RELU_INPUT ? x : nullptr, ldx};
+  return run_expand(Expand{dy, lddy, w, ldw, n, a->in, a->out, nullptr, dx, lddx, a->precision, lr}, e == 2, false,
+                    wk.part, st);
 } catch (const std::bad_alloc&) {
   return ot::set_error(OT_E_NOMEM, "adapters_backward: out of host memory");
 }

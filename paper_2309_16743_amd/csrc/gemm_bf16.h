@@ -27,6 +27,7 @@
 
 #include "adam.h"
 #include "common.h"
+#include "lowrank_ops.h"
 
 namespace ot {
 
@@ -58,9 +59,15 @@ enum class EpiB : int {
   BiasReluBf = 3, // C (bf16) = bf16(max(acc + bias[n], 0))
   MaskBf = 4,     // C (bf16) = bf16(acc * (mask[m, n] > 0)), mask bf16
   MseBf = 5,      // R = acc + bias[n] - T[m, n] (T fp32); C (bf16) = bf16(scale R); per-block sum of R^2
-  AdamF32 = 6     // acc is the gradient of the fp32 master weights C: Adam updates C, adam_m, adam_v
+  AdamF32 = 6,    // acc is the gradient of the fp32 master weights C: Adam updates C, adam_m, adam_v
                   // (same layout as C) and writes bf16(C) to adam_pb; no gradient is stored
+  // Low-rank adapters (adapters.hip): A's row m is row lr.perm[m] in memory, acc gains the rows'
+  // low-rank product (split 0), K may have any length
+  AdaptF32 = 7,   // C (fp32) row perm[m] = acc (+ bias[n]) (ReLU)
+  AdaptBf = 8,    // C (bf16) row perm[m] = bf16(acc (+ bias[n]) (ReLU, or 0 where lr.mask is not above 0))
+  AdaptSplit = 9  // C (fp32)[split] row m = acc
 };
+constexpr bool is_adapt(EpiB e) { return e == EpiB::AdaptF32 || e == EpiB::AdaptBf || e == EpiB::AdaptSplit; }
 
 struct GemmBArgs {
   const uint16_t* A;
@@ -89,6 +96,7 @@ struct GemmBArgs {
   float* adam_v;
   uint16_t* adam_pb;
   AdamArgs adam;
+  AdaptRows lr;             // Adapt*
 };
 
 __device__ __forceinline__ int64_t xcd_remap_b(int64_t p, int64_t g) {
@@ -117,6 +125,12 @@ __device__ __forceinline__ void load_target_rows(const GemmBArgs& g, int64_t m0,
     }
 }
 
+// Row numbers of the tile's sorted rows (Adapt*).
+template <int BM>
+__device__ __forceinline__ void load_adapt_rows(const GemmBArgs& g, int64_t m0, int32_t* s_trow) {
+  for (int i = threadIdx.x; i < BM; i += blockDim.x) s_trow[i] = g.lr.perm[min(m0 + i, g.M - 1)];
+}
+
 template <int WN, EpiB EPI, int NW = 4>
 struct BEpi {
   static constexpr int EP = WN + 4;
@@ -127,6 +141,7 @@ struct BEpi {
   bool cfull;
   const int32_t* s_trow = nullptr;   // MseBf with target_rows: row indices of the tile (LDS), row tile_m0 first
   int64_t tile_m0 = 0;
+  bool odd = false;                  // Adapt*: values that are not finite were left out of the low-rank product
   __device__ __forceinline__ int64_t trow(const GemmBArgs& g, int64_t m) const {
     return g.target_rows ? (int64_t)s_trow[m - tile_m0] : m;
   }
@@ -148,6 +163,10 @@ struct BEpi {
         for (int c = 0; c < 4; ++c) bias4[c] = (col + c < g.N) ? g.bias[col + c] : 0.f;
       }
     }
+    if constexpr (EPI == EpiB::AdaptF32 || EPI == EpiB::AdaptBf) {       // the caller's bias: any alignment
+      if (g.bias)
+        for (int c = 0; c < 4; ++c) bias4[c] = (col + c < g.N) ? g.bias[col + c] : 0.f;
+    }
   }
 
   // Rows m0 .. m0 + ROWS - 1 (ep row 0 = row m0).  stage() writes the chunk's
@@ -158,6 +177,10 @@ struct BEpi {
     constexpr int NP = ROWS / RPP;
     if constexpr (EPI == EpiB::AdamF32) {
       adam_rows<NP>(g, ep, m0, stage);
+      return;
+    }
+    if constexpr (is_adapt(EPI)) {
+      adapt_rows<NP>(g, ep, m0, split, stage);
       return;
     }
     // targets (MseBf) or mask (MaskBf) of each pass; one branch around all
@@ -229,6 +252,71 @@ struct BEpi {
         } else {
           for (int c = 0; c < 4; ++c)
             if (col + c < g.N) C[c] = h4[c];
+        }
+      }
+    }
+  }
+
+  // Adapt*: the products with values of the row's own adapter that are not finite.
+  __device__ __forceinline__ void add_odd(const GemmBArgs& g, int64_t m, float (&v)[4]) const {
+    const int a = g.lr.gid[m];
+    if (a >= g.lr.G) return;
+    for (int r = 0; r < g.lr.R; ++r) {
+      const uint16_t* p = static_cast<const uint16_t*>(g.lr.mat) + ((int64_t)a * g.lr.R + r) * g.lr.ldm + col;
+      for (int c = 0; c < 4; ++c) {
+        const float x = col + c < g.N ? bf2f(p[c]) : 0.f;
+        if (!(fabsf(x) <= 3.402823466e38f)) v[c] = fmaf(g.lr.ts[m * g.lr.RP + r], x, v[c]);
+      }
+    }
+  }
+
+  // Adapt*: rows scattered to their numbers (s_trow); the masks of a chunk are read together, before it is staged.
+  template <int NP, class Stage>
+  __device__ __forceinline__ void adapt_rows(const GemmBArgs& g, const float* ep, int64_t m0, int64_t split,
+                                             Stage stage) {
+    const bool masked = EPI == EpiB::AdaptBf && g.lr.mask != nullptr;
+    u16x4 pre[NP];
+    if (masked) {
+      const uint16_t* mask = static_cast<const uint16_t*>(g.lr.mask);
+      const int64_t c = min(col, (g.N - 1) / 4 * 4);      // rows are padded to whole 16-byte pieces
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        pre[i] = *reinterpret_cast<const u16x4*>(mask + (int64_t)s_trow[m0 - tile_m0 + rl + RPP * i] * g.lr.ldmask + c);
+    }
+    stage();
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int rr = rl + RPP * i;
+      const int64_t m = m0 + rr;
+      if (m >= g.M || col >= g.N) continue;
+      const f32x4 a4 = *reinterpret_cast<const f32x4*>(ep + rr * EP + 4 * cg);
+      float v[4] = {a4[0], a4[1], a4[2], a4[3]};
+      if (odd) add_odd(g, m, v);
+      if constexpr (EPI == EpiB::AdaptSplit) {
+        // sorted rows of a workspace whose rows are padded to whole vectors
+        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(g.C) + split * g.split_stride + m * g.ldc + col) =
+            f32x4{v[0], v[1], v[2], v[3]};
+      } else {
+        const int64_t row = s_trow[m - tile_m0];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          v[c] += bias4[c];
+          if (g.lr.relu) v[c] = v[c] < 0.f ? 0.f : v[c];          // NaN stays
+          if (masked) v[c] = bf2f(pre[i][c]) > 0.f ? v[c] : 0.f;
+        }
+        if constexpr (EPI == EpiB::AdaptF32) {
+          float* C = reinterpret_cast<float*>(g.C) + row * g.ldc + col;
+          if (cfull) *reinterpret_cast<f32x4*>(C) = f32x4{v[0], v[1], v[2], v[3]};
+          else
+            for (int c = 0; c < 4; ++c)
+              if (col + c < g.N) C[c] = v[c];
+        } else {
+          uint16_t* C = reinterpret_cast<uint16_t*>(g.C) + row * g.ldc + col;
+          const u16x4 h = {lr_bf16(v[0]), lr_bf16(v[1]), lr_bf16(v[2]), lr_bf16(v[3])};
+          if (cfull) *reinterpret_cast<u16x4*>(C) = h;
+          else
+            for (int c = 0; c < 4; ++c)
+              if (col + c < g.N) C[c] = h[c];
         }
       }
     }
@@ -671,6 +759,120 @@ __device__ __forceinline__ void frag_fence_regs(bf16x8 (&x)[N]) {
   }
 }
 
+// stage_offsets of a KMajor A whose rows are taken through lr.perm.
+template <int TILE, int BK, int NW, int N>
+__device__ __forceinline__ void adapt_offsets(int64_t (&off)[N], int wid, int lane, int64_t x0, const GemmBArgs& g) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int ci = (i * NW + wid) * 64 + lane;
+    constexpr int KC = BK / 8;
+    const int row = ci / KC, pc = ci % KC, lc = pc ^ kswz<BK>(row);
+    off[i] = (int64_t)g.lr.perm[min(x0 + row, g.M - 1)] * g.lda + 8 * lc;
+  }
+}
+
+// What the main loop leaves out of a wavefront's sums (Adapt*, 32 x 32
+// fragments, rows mw.., columns nw..): the columns [k0, k1) past its whole k tiles, and
+// (lowrank) the rows' low-rank products.  Both come straight from memory: a
+// tile's low-rank part is rank / K of its work plus one step per adapter that
+// its rows name.  Rows of other adapters enter an adapter's product as zeros;
+// so that its infinities and NaN do not reach them, those enter as zeros too, and the
+// return value (the same for the whole wavefront) says that the epilogue has to add their
+// products to the rows they belong to (BEpi::add_odd).  The fp32 low-rank values enter as TERMS bf16 terms: two leave 2^-18 of
+// them (a bf16 result), three 2^-27 (fp32).
+template <int FM, int FN, LayB LB, int TERMS, class Acc>
+__device__ __forceinline__ bool adapt_extra(const GemmBArgs& g, Acc (&acc)[FM][FN], int64_t mw, int64_t nw,
+                                            bool lowrank, int64_t k0, int64_t k1, int lane) {
+  const int i = lane % 32, kg = 8 * (lane / 32);
+  auto frag = [](lr_u32x4 v) { return __builtin_bit_cast(bf16x8, v); };
+  // 8 values of column n from rows r0 + kg .. of `rows` rows of a matrix with row stride ld: the
+  // wavefront-wide row r0 + e is a scalar base, the lane adds its half's 8 rows and its column
+  // (below 2^31: ld and n are at most 2^26 + 8)
+  auto column = [&](const uint16_t* p, int64_t ld, int64_t r0, int64_t rows, int64_t n) {
+    const uint32_t far = (uint32_t)(kg * ld + n), near = (uint32_t)n;
+    lr_u32x4 v{};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t h[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int64_t r = r0 + 2 * w + e;
+        const bool in = r + kg < rows;
+        const uint16_t* row = p + min(r, rows - 1) * ld;     // uniform
+        const uint32_t t = row[in ? far : near];
+        h[e] = in ? t : 0u;
+      }
+      v[w] = h[0] | (h[1] << 16);
+    }
+    return v;
+  };
+  for (int64_t k = k0; k < k1; k += 16) {
+    bf16x8 b[FN];
+#pragma unroll
+    for (int h = 0; h < FN; ++h) {
+      const int64_t n = min(nw + 32 * h + i, g.N - 1);
+      if constexpr (LB == LayB::KMajor) b[h] = frag(lr_load16(g.B + n * g.ldb + k + kg, k1 - k - kg));
+      else b[h] = frag(column(g.B, g.ldb, k, k1, n));
+    }
+#pragma unroll
+    for (int f = 0; f < FM; ++f) {
+      const bf16x8 a =
+          frag(lr_load16(g.A + (int64_t)g.lr.perm[min(mw + 32 * f + i, g.M - 1)] * g.lda + k + kg, k1 - k - kg));
+#pragma unroll
+      for (int h = 0; h < FN; ++h) acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[h], acc[f][h], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);       // one fragment's operands in registers at a time
+    }
+  }
+  uint32_t odd = 0;
+  if (!lowrank) return false;
+  const int64_t me = min(mw + 32 * FM, g.M);
+  for (int64_t p = mw; p < me;) {
+    const int a = __builtin_amdgcn_readfirstlane(g.lr.gid[p]);
+    if (a >= g.lr.G) break;                              // rows without an adapter come last
+    const int64_t s0 = g.lr.off[a], s1 = g.lr.off[a + 1];
+    const uint16_t* mat = static_cast<const uint16_t*>(g.lr.mat) + (int64_t)a * g.lr.R * g.lr.ldm;
+    for (int rc = 0; rc < g.lr.RP; rc += 16) {
+      bf16x8 b[FN];
+#pragma unroll
+      for (int h = 0; h < FN; ++h) {
+        lr_u32x4 v = column(mat, g.lr.ldm, rc, g.lr.R, min(nw + 32 * h + i, g.N - 1));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t lo = (v[w] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
+          const uint32_t hi = (v[w] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+          odd |= lo | hi;
+          v[w] &= ~(lo | hi);
+        }
+        b[h] = frag(v);
+      }
+#pragma unroll
+      for (int f = 0; f < FM; ++f) {
+        const int64_t row = mw + 32 * f + i;
+        if (max(s0, mw + 32 * f) >= min(s1, mw + 32 * f + 32)) continue;   // the same for the whole wavefront
+        float x[8];
+        const bool in = row >= s0 && row < s1;
+        const f32x4* src = reinterpret_cast<const f32x4*>(g.lr.ts + (in ? row : s0) * g.lr.RP + rc + kg);
+        const f32x4 lo = src[0], hi = src[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = in ? lo[e] : 0.f;
+          x[4 + e] = in ? hi[e] : 0.f;
+        }
+        lr_u32x4 t[TERMS];
+        lr_split8<TERMS>(x, t);
+#pragma unroll
+        for (int h = 0; h < FN; ++h)
+#pragma unroll
+          for (int z = TERMS - 1; z >= 0; --z)
+            acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(t[z]), b[h], acc[f][h], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);               // one fragment's operands in registers at a time
+      }
+    }
+    p = s1;
+  }
+  return __ballot(odd != 0) != 0;
+}
+
 template <int BM, int BN, int BK, int S, int OCC, LayB LA, LayB LB, EpiB EPI, int NWN = 2>
 __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArgs g) {
   constexpr int NW = 2 * NWN, NT = 64 * NW;                       // 2 x NWN wavefronts
@@ -690,7 +892,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   static_assert(CH_F >= 1 && NW * CH_F * 32 * EP * 4 <= S * STAGE_BYTES, "epilogue staging");
   __shared__ __attribute__((aligned(16))) unsigned char smem[S * STAGE_BYTES];
   __shared__ double s_red[8 + NW * WN / 2];
-  __shared__ int32_t s_trow[EPI == EpiB::MseBf ? BM : 1];
+  __shared__ int32_t s_trow[EPI == EpiB::MseBf || is_adapt(EPI) ? BM : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int wm = wid % 2, wn = wid / 2;
@@ -708,9 +910,11 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow);
 
   int64_t a_off[LA_N], b_off[LB_N];
-  stage_offsets<LA, BM, BK, NW>(a_off, wid, lane, m0, g.M, g.lda);
+  if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
+  else stage_offsets<LA, BM, BK, NW>(a_off, wid, lane, m0, g.M, g.lda);
   stage_offsets<LB, BN, BK, NW>(b_off, wid, lane, n0, g.N, g.ldb);
   // k tile kt into stage st
   auto issue = [&](int kt, int st) {
@@ -800,14 +1004,20 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
 #undef OT_WAIT_VM
   static_assert(S <= 4, "wait depth");
 
+  bool odd = false;
+  if constexpr (is_adapt(EPI))
+    odd = adapt_extra<FM, FN, LB, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, m0 + WM * wm, n0 + WN * wn, split == 0,
+                                                                 kbeg + (int64_t)nk * BK, kend, lane);
+
   // Epilogue in FM / CH_F chunks of 32 CH_F rows per wave, staged through the
   // (now free) stage buffers.
   float* ep = reinterpret_cast<float*>(smem) + wid * (CH_F * 32 * EP);
   BEpi<WN, EPI, NW> e(g, n0 + WN * wn);
-  if constexpr (EPI == EpiB::MseBf) {
+  if constexpr (EPI == EpiB::MseBf || is_adapt(EPI)) {
     if (nk == 0) lds_barrier();        // publishes s_trow (the main loop's barriers do otherwise)
     e.s_trow = s_trow;
     e.tile_m0 = m0;
+    e.odd = odd;
   }
 #pragma unroll
   for (int c0 = 0; c0 < FM; c0 += CH_F) {
@@ -867,7 +1077,7 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   static_assert(S >= 3 && S <= 4, "stages");
   __shared__ __attribute__((aligned(16))) unsigned char smem[S * STAGE_BYTES];
   __shared__ double s_red[8 + NW * WN / 2];
-  __shared__ int32_t s_trow[EPI == EpiB::MseBf ? BM : 1];
+  __shared__ int32_t s_trow[EPI == EpiB::MseBf || is_adapt(EPI) ? BM : 1];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -885,9 +1095,11 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow);
 
   int64_t a_off[LA_N], b_off[LB_N];
-  stage_offsets<LA, BM, BK, NW>(a_off, wid, lane, m0, g.M, g.lda);
+  if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
+  else stage_offsets<LA, BM, BK, NW>(a_off, wid, lane, m0, g.M, g.lda);
   stage_offsets<LB, BN, BK, NW>(b_off, wid, lane, n0, g.N, g.ldb);
   auto issue = [&](int kt) {
     const int64_t k0 = kbeg + (int64_t)kt * BK;
@@ -974,12 +1186,17 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
     }
   }
 #undef OT_WAIT_VM
+  bool odd = false;
+  if constexpr (is_adapt(EPI))
+    odd = adapt_extra<FM, FN, LB, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, m0 + WM * wm, n0 + WN * wn, split == 0,
+                                                                 kbeg + (int64_t)nk * BK, kend, lane);
 
   float* ep = reinterpret_cast<float*>(smem) + wid * (CH_F * 32 * EP);
   BEpi<WN, EPI, NW> e(g, n0 + WN * wn);
-  if constexpr (EPI == EpiB::MseBf) {
+  if constexpr (EPI == EpiB::MseBf || is_adapt(EPI)) {
     e.s_trow = s_trow;
     e.tile_m0 = m0;
+    e.odd = odd;
   }
 #pragma unroll
   for (int c0 = 0; c0 < FM; c0 += CH_F) {

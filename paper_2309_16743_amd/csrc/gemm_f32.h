@@ -26,6 +26,7 @@
 
 #include "adam.h"
 #include "common.h"
+#include "lowrank_ops.h"
 
 namespace ot {
 
@@ -37,8 +38,14 @@ enum class Epi : int {
   Mse = 3,       // Y = acc + bias[n]; R = Y - T; C = scale * R; partial sum of R^2 per block
   SplitK = 4,    // C[split] = acc (partial sums, reduced by a separate pass)
   Mask = 5,      // C = acc * (mask[m, n] > 0)
-  Adam = 6       // acc is the gradient of the weights C: Adam updates C, adam_m, adam_v (same layout as C)
+  Adam = 6,      // acc is the gradient of the weights C: Adam updates C, adam_m, adam_v (same layout as C)
+  // Low-rank adapters (adapters.hip; gemm_f32x3_kernel only): A's row m is row lr.perm[m] in memory, acc
+  // gains the rows' low-rank product (split 0)
+  AdaptF32 = 7,  // C (fp32) row perm[m] = acc (+ bias[n]) (ReLU, or 0 where lr.mask is not above 0)
+  AdaptBf = 8,   // C (bf16) row perm[m] = the same, rounded
+  AdaptSplit = 9 // C[split] row m = acc
 };
+constexpr bool is_adapt(Epi e) { return e == Epi::AdaptF32 || e == Epi::AdaptBf || e == Epi::AdaptSplit; }
 
 struct GemmArgs {
   const float* A;
@@ -70,6 +77,7 @@ struct GemmArgs {
   float* bias_m;            //   updated by the thread that has its sum
   float* bias_v;
   AdamArgs adam;
+  AdaptRows lr;             // Adapt*
 };
 
 // Row sum of row m (the bias gradient) to where it goes; Adam on the bias element.

@@ -118,13 +118,16 @@ struct X3Operand {
   static __device__ __forceinline__ int row_at(int r) { return PERM ? (r * 32) ^ (((r >> 5) & 1) << 7) : r * 32; }
   static __device__ __forceinline__ bool mine(int i) { return CHUNKS % 256 == 0 || (int)threadIdx.x + i * 256 < CHUNKS; }
 
-  __device__ __forceinline__ X3Operand(const float* p, int64_t ld_, int64_t x0, int64_t lim) : base(p), ld(ld_) {
+  // perm (KMajor, nullable): row r of the operand is row perm[r] in memory
+  __device__ __forceinline__ X3Operand(const float* p, int64_t ld_, int64_t x0, int64_t lim,
+                                       const int32_t* perm = nullptr) : base(p), ld(ld_) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int ci = mine(i) ? threadIdx.x + i * 256 : 0;      // threads without a chunk load the first
       if constexpr (L == Lay::KMajor) {
         // rows past the operand read its last one; their results are not stored
-        off[i] = min(x0 + ci / 2, lim - 1) * ld + 8 * (ci % 2);
+        const int64_t r = min(x0 + ci / 2, lim - 1);
+        off[i] = (perm ? (int64_t)perm[r] : r) * ld + 8 * (ci % 2);
         cnt[i] = 8;
       } else {
         const int64_t c = x0 + 8 * (ci % (T / 8));
@@ -165,8 +168,16 @@ struct X3Operand {
   }
   __device__ __forceinline__ void store(unsigned char* lds, float& big) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (!mine(i)) continue;
+    for (int i = 0; i < N; ++i) store_chunk(i, lds, big);
+  }
+  // largest value per chunk (of one row each, KMajor)
+  __device__ __forceinline__ void store(unsigned char* lds, float (&big)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) store_chunk(i, lds, big[i]);
+  }
+  __device__ __forceinline__ void store_chunk(int i, unsigned char* lds, float& big) const {
+    {
+      if (!mine(i)) return;
       const int ci = threadIdx.x + i * 256;
       const float x[8] = {v[i][0][0], v[i][0][1], v[i][0][2], v[i][0][3],
                           v[i][1][0], v[i][1][1], v[i][1][2], v[i][1][3]};
@@ -232,6 +243,66 @@ constexpr int x3_waves(int wgn, int fm, int fn) { return (wgn == 4 || fm * fn >=
 // are meant to stay in flight.
 __device__ __forceinline__ void x3_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Low-rank products of a wavefront's rows mw.. (Adapt*), col(h): this lane's column
+// of fragment h: fp32 matrix instructions on the fp32 values, straight from memory
+// (rank / K of the tile's work).  Rows of other adapters enter as zeros, and an
+// adapter's infinities and NaN too, so that they do not reach them; the return value (the
+// same for the whole wavefront) says that their products are still to be added (adapt_odd_f32).
+template <int FM, int FN, class Col>
+__device__ __forceinline__ bool adapt_lowrank_f32(const GemmArgs& g, x3_f32x16 (&acc)[FM][FN], int64_t mw, Col col) {
+  const int lane = threadIdx.x & 63, i = lane % 32, half = lane / 32;
+  const int64_t me = min(mw + 32 * FM, g.M);
+  bool odd = false;
+  for (int64_t p = mw; p < me;) {
+    const int a = __builtin_amdgcn_readfirstlane(g.lr.gid[p]);
+    if (a >= g.lr.G) break;                              // rows without an adapter come last
+    const int64_t s0 = g.lr.off[a], s1 = g.lr.off[a + 1];
+    const float* mat = static_cast<const float*>(g.lr.mat) + (int64_t)a * g.lr.R * g.lr.ldm;
+    for (int rc = 0; rc < g.lr.RP; rc += 16) {
+      float b[FN][8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int r = min(rc + 2 * q + half, g.lr.R - 1);   // ranks past R meet zeros of ts
+#pragma unroll
+        for (int h = 0; h < FN; ++h) {
+          const float v = mat[(int64_t)r * g.lr.ldm + col(h)];
+          const bool bad = !(fabsf(v) <= 3.402823466e38f);
+          odd |= bad;
+          b[h][q] = bad ? 0.f : v;
+        }
+      }
+#pragma unroll
+      for (int f = 0; f < FM; ++f) {
+        const int64_t row = mw + 32 * f + i;
+        if (max(s0, mw + 32 * f) >= min(s1, mw + 32 * f + 32)) continue;   // the same for the whole wavefront
+        const bool in = row >= s0 && row < s1;
+        const float* ts = g.lr.ts + (in ? row : s0) * g.lr.RP + rc + half;
+        float x[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = ts[2 * q];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+#pragma unroll
+          for (int h = 0; h < FN; ++h)
+            acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x[q] : 0.f, b[h][q], acc[f][h], 0, 0, 0);
+      }
+    }
+    p = s1;
+  }
+  return __ballot(odd) != 0;
+}
+
+// x with the products of sorted row m's own adapter whose value is not finite.
+__device__ __forceinline__ float adapt_odd_f32(const GemmArgs& g, int64_t m, int64_t n, float x) {
+  const int a = g.lr.gid[m];
+  if (a >= g.lr.G) return x;
+  for (int r = 0; r < g.lr.R; ++r) {
+    const float v = static_cast<const float*>(g.lr.mat)[((int64_t)a * g.lr.R + r) * g.lr.ldm + n];
+    if (!(fabsf(v) <= 3.402823466e38f)) x = fmaf(g.lr.ts[m * g.lr.RP + r], v, x);
+  }
+  return x;
+}
+
 template <int WGM, int WGN, int FM, int FN, Lay LA, Lay LB, Epi EPI, int ROLE = 0>
 __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(GemmArgs g) {
   static_assert(WGM * WGN == 4, "four wavefronts");
@@ -243,7 +314,9 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
   __shared__ __attribute__((aligned(16))) unsigned char smem[2 * BUF];
   __shared__ int s_huge;
   __shared__ double s_red[4];
-  __shared__ int32_t s_trow[EPI == Epi::Mse ? BM : 1];
+  constexpr bool AD = is_adapt(EPI);
+  __shared__ int32_t s_trow[EPI == Epi::Mse || AD ? BM : 1];
+  __shared__ int s_hrow[AD ? BM : 1];                    // Adapt*: rows of A to sum again
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -273,9 +346,15 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
       s_trow[tid] = (int32_t)min(max((int64_t)g.target_rows[m], (int64_t)0), g.target_rows_max);
     }
   }
+  if constexpr (AD) {
+    if (tid < BM) {
+      s_trow[tid] = g.lr.perm[min(m0 + tid, g.M - 1)];
+      s_hrow[tid] = 0;
+    }
+  }
   x3_barrier();
 
-  OA oa(g.A, g.lda, m0, g.M);
+  OA oa(g.A, g.lda, m0, g.M, AD ? g.lr.perm : nullptr);
   OB ob(g.B, g.ldb, n0, g.N);
   x3_f32x16 acc[FM][FN];
 #pragma unroll
@@ -347,9 +426,13 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
   auto col_of = [&](int h) { return nw + (IL ? h : 32 * h); };
   float big_a = 0.f, big_kb = 0.f;                       // largest |value| this thread has split, or NaN
   float& big_b = LA == LB ? big_a : big_kb;              // (the maximum of a KMajor operand would drop the NaN)
+  float big_row[AD ? OA::N : 1];
+#pragma unroll
+  for (int i = 0; i < (AD ? OA::N : 1); ++i) big_row[i] = 0.f;
   auto store = [&](int buf) {
     add_rowsum();
-    oa.store(smem + buf * BUF, big_a);
+    if constexpr (AD) oa.store(smem + buf * BUF, big_row);
+    else oa.store(smem + buf * BUF, big_a);
     ob.store(smem + buf * BUF + OA::BYTES, big_b);
   };
   int64_t t = 0;
@@ -382,13 +465,30 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
 #pragma unroll
     for (int h = 0; h < FN; ++h) acc[f][h] += low[f][h];
 
-  if (!(big_a < kX3Huge && big_b < kX3Huge)) s_huge = 1;
+  // Adapt*: a batch's rows are independent of each other, so only the rows of A with such
+  // values are summed again (bit 1 of s_huge), or all rows when B has them (bit 0)
+  if constexpr (!AD) {
+    if (!(big_a < kX3Huge && big_b < kX3Huge)) s_huge = 1;
+  } else {
+    if (!(big_b < kX3Huge)) atomicOr(&s_huge, 1);
+#pragma unroll
+    for (int i = 0; i < OA::N; ++i)
+      if (OA::mine(i) && !(big_row[i] < kX3Huge)) {
+        s_hrow[(tid + i * 256) / 2] = 1;
+        atomicOr(&s_huge, 2);
+      }
+  }
   x3_barrier();
-  if (__builtin_amdgcn_readfirstlane(s_huge)) {            // the same for the whole block
+  const int huge = __builtin_amdgcn_readfirstlane(s_huge);   // the same for the whole block
+  if (huge) {
+    // (low is free: Adapt* keeps in it the sums of the rows that need no second pass)
 #pragma unroll
     for (int f = 0; f < FM; ++f)
 #pragma unroll
-      for (int h = 0; h < FN; ++h) acc[f][h] = x3_f32x16{};
+      for (int h = 0; h < FN; ++h) {
+        if constexpr (AD) low[f][h] = acc[f][h];
+        acc[f][h] = x3_f32x16{};
+      }
     float* fa = reinterpret_cast<float*>(smem);           // [16][BM], then [16][BN]
     float* fb = fa + 16 * BM;
     static_assert(64 * (BM + BN) <= 2 * BUF, "fp32 tile");
@@ -416,7 +516,22 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
       }
     }
     x3_barrier();
+    if constexpr (AD) {
+      if (!(huge & 1)) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const bool again = s_hrow[(int)(row_of(f, r) - m0)] != 0;
+#pragma unroll
+            for (int h = 0; h < FN; ++h) acc[f][h][r] = again ? acc[f][h][r] : low[f][h][r];
+          }
+      }
+    }
   }
+  bool odd = false;
+  if constexpr (AD)
+    if (split == 0) odd = adapt_lowrank_f32<FM, FN>(g, acc, m0 + WM * wm, [&](int h) { return min(col_of(h), g.N - 1); });
   if constexpr (LA == Lay::MNMajor) {
     if (do_rowsum) {                                      // uniform over the block
       float* red = reinterpret_cast<float*>(smem);        // [16][BM]
@@ -437,7 +552,7 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
   }
 
   // ---------------------------------------------------------------- epilogue
-  float* Cb = g.C + (EPI == Epi::SplitK ? split * g.split_stride : 0);
+  float* Cb = g.C + (EPI == Epi::SplitK || EPI == Epi::AdaptSplit ? split * g.split_stride : 0);
   const bool full = col_of(FN - 1) < g.N;
   // this lane's FN values of a row starting at p (column 0 of the row)
   auto get = [&](const float* p, float* out) {
@@ -516,6 +631,52 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    return;
+  }
+  if constexpr (AD) {
+    constexpr bool BF = EPI == Epi::AdaptBf;
+    const float* mask = EPI == Epi::AdaptSplit ? nullptr : static_cast<const float*>(g.lr.mask);
+#pragma unroll
+    for (int h = 0; h < FN; ++h) bias[h] = EPI != Epi::AdaptSplit && g.bias && col_of(h) < g.N ? g.bias[col_of(h)] : 0.f;
+#pragma unroll
+    for (int f = 0; f < FM; ++f) {
+      float pre[16][FN];
+      if (mask) {
+#pragma unroll
+        for (int u = 0; u < 16; ++u) get(mask + (int64_t)s_trow[(int)(row_of(f, u) - m0)] * g.lr.ldmask, pre[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const int64_t m = row_of(f, u);
+        if (m >= g.M) continue;
+        float val[FN];
+#pragma unroll
+        for (int h = 0; h < FN; ++h) {
+          float x = acc[f][h][u];
+          if (odd && col_of(h) < g.N) x = adapt_odd_f32(g, m, col_of(h), x);
+          if constexpr (EPI != Epi::AdaptSplit) {
+            x += bias[h];
+            if (g.lr.relu) x = x < 0.f ? 0.f : x;           // NaN stays
+            if (mask && !(pre[u][h] > 0.f)) x = 0.f;
+          }
+          val[h] = x;
+        }
+        if constexpr (EPI == Epi::AdaptSplit) {
+          put(Cb + m * g.ldc, val);
+        } else if constexpr (BF) {
+          uint16_t* C = reinterpret_cast<uint16_t*>(g.C) + (int64_t)s_trow[(int)(m - m0)] * g.ldc;
+          if (IL && full) {
+            *reinterpret_cast<uint32_t*>(C + nw) = (uint32_t)lr_bf16(val[0]) | ((uint32_t)lr_bf16(val[FN - 1]) << 16);
+          } else {
+#pragma unroll
+            for (int h = 0; h < FN; ++h)
+              if (col_of(h) < g.N) C[col_of(h)] = lr_bf16(val[h]);
+          }
+        } else {
+          put(g.C + (int64_t)s_trow[(int)(m - m0)] * g.ldc, val);
+        }
+      }
     }
     return;
   }

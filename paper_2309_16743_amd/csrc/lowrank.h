@@ -16,6 +16,7 @@
 
 #include "common.h"
 #include "intmath.h"
+#include "lowrank_ops.h"
 
 namespace ot {
 
@@ -25,38 +26,6 @@ constexpr int kSlotRows = 32;       // sorted rows of one adapter that a block t
 struct RowSlot {
   int32_t start, count, g, pad;
 };
-
-typedef __bf16 lr_bf16x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t lr_u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t lr_u32x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ float lr_value(const float* p) { return *p; }
-__device__ __forceinline__ float lr_value(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-// round to nearest even, NaN stays NaN
-__device__ __forceinline__ uint16_t lr_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
-__device__ __forceinline__ void lr_store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void lr_store(uint16_t* p, float v) { *p = lr_bf16(v); }
-
-// 16 bytes at p of which the first `valid` elements (of 2 or 4 bytes) exist, zeros past them.  The
-// piece is 16-byte aligned, so it may be read whole if one element exists.
-template <class T>
-__device__ __forceinline__ lr_u32x4 lr_load16(const T* p, int64_t valid) {
-  constexpr int V = 16 / (int)sizeof(T);
-  if (valid <= 0) return lr_u32x4{0, 0, 0, 0};
-  lr_u32x4 q = *reinterpret_cast<const lr_u32x4*>(p);
-  if (valid < V) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if constexpr (sizeof(T) == 2) {
-        if (2 * w >= valid) q[w] = 0;
-        else if (2 * w + 1 >= valid) q[w] &= 0xffffu;
-      } else {
-        if (w >= valid) q[w] = 0;
-      }
-    }
-  }
-  return q;
-}
 
 // D += A B with the 16 bytes that lane l holds of each operand as its k values.
 template <class T>
@@ -70,32 +39,6 @@ __device__ __forceinline__ f32x4 lr_mfma(lr_u32x4 a, lr_u32x4 b, f32x4 d) {
       d = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), d, 0, 0, 0);
     return d;
   }
-}
-
-// x as a sum of TERMS bf16 values, packed in pairs: t[q] holds term q of 8 values.
-// Two terms leave 2^-18 of x, three 2^-27.  Infinities and NaN: the first term
-// holds them, later ones are zero (inf - inf would be NaN).
-template <int TERMS>
-__device__ __forceinline__ void lr_split8(const float (&x)[8], lr_u32x4 (&t)[TERMS]) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  float rest[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) rest[e] = x[e];
-#pragma unroll
-  for (int q = 0; q < TERMS; ++q)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const bf16x2 h = __builtin_convertvector(f32x2{rest[2 * w], rest[2 * w + 1]}, bf16x2);
-      t[q][w] = __builtin_bit_cast(uint32_t, h);
-      if (q + 1 < TERMS) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float hi = __uint_as_float(e ? (t[q][w] & 0xffff0000u) : (t[q][w] << 16));
-          const float r = rest[2 * w + e] - hi;
-          rest[2 * w + e] = fabsf(hi) <= 3.402823466e38f ? r : 0.f;
-        }
-      }
-    }
 }
 
 // ------------------------------------------------------------------ shrink
