@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "adapters.h"
@@ -23,11 +24,12 @@ namespace ot {
 // order: it counts the rows of smaller keys, which is where its own start, and
 // then writes them.  Every block reads all ids (n G / 64 wavefront reads from
 // the caches) and none waits for another.  Slots: adapter g's first is
-// start / kSlotRows + g, which leaves room for those of the adapters before it; those
+// start / slot_rows + g, which leaves room for those of the adapters before it; those
 // that stay unused get count 0.
 __global__ __launch_bounds__(256) void group_rows_kernel(const int32_t* __restrict__ ids, int32_t n, int32_t G,
                                                          int32_t* __restrict__ perm, int32_t* __restrict__ gid,
-                                                         int32_t* __restrict__ off, RowSlot* __restrict__ slots) {
+                                                         int32_t* __restrict__ off, RowSlot* __restrict__ slots,
+                                                         int32_t slot_rows) {
   __shared__ int32_t s_less[4], s_same[4];
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   auto key = [&](int i) {
@@ -55,10 +57,10 @@ __global__ __launch_bounds__(256) void group_rows_kernel(const int32_t* __restri
     off[g] = start;
     if (g == G) off[G + 1] = n;
   }
-  const int slot0 = start / kSlotRows + g, slot1 = (start + count) / kSlotRows + g + 1;
+  const int slot0 = start / slot_rows + g, slot1 = (start + count) / slot_rows + g + 1;
   for (int s = slot0 + tid; s < slot1; s += 256) {
-    const int r = (s - slot0) * kSlotRows;
-    slots[s] = RowSlot{start + r, max(0, min(kSlotRows, count - r)), g, 0};
+    const int r = (s - slot0) * slot_rows;
+    slots[s] = RowSlot{start + r, max(0, min(slot_rows, count - r)), g, 0};
   }
   int at = start;
   for (int i0 = 0; i0 < n && at < start + count; i0 += 256) {   // the same for all threads: at is uniform
@@ -195,6 +197,14 @@ Plan plan_expand(bool bf16, bool kmajor, int64_t M, int64_t N, int64_t K) {
 // Partial sums of the plan (fp32 values; 0: not split).
 int64_t plan_values(const Plan& p, int64_t M, int64_t N) { return p.splits > 1 ? p.splits * M * ((N + 3) / 4 * 4) : 0; }
 
+// Pieces of 64 columns per wavefront in the one pass over a long dy (0: dy is short and
+// takes the two products apart).
+int pass_chunks(int64_t L, int32_t G) {
+  if (L < 65536) return 0;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(4, L / 512 * G / 1024));
+}
+int64_t pass_ranges(int64_t L, int32_t G) { return ot::ceil_div(L, (int64_t)pass_chunks(L, G) * ot::kPassThreads); }
+
 struct Work {
   int32_t* perm;
   int32_t* gid;
@@ -205,12 +215,20 @@ struct Work {
   int64_t n_slots;
 };
 
+constexpr int kMinSlotRows = 16;
+
+// Rows of a slot for a product over L values: short ranges are not split, so smaller slots
+// give the blocks that fill the card (1024 rows of 2048 values: 9.3 us with 16, 11.5 with 32); long ones
+// read the adapter's matrix once per slot.
+int slot_rows(int64_t L) { return L <= 4096 ? kMinSlotRows : ot::kSlotRows; }
+
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 // Partial sums that a call of up to n rows needs.
 int64_t part_values(const ot_adapters* a, int64_t n) {
   // shrinks: splits * rows, with splits <= kShrinkBlocks / (rows / 32) + 1
   int64_t most = std::max(a->in, a->out) > 4096 ? (kShrinkBlocks * ot::kSlotRows + n) * a->RP : 0;
+  if (pass_chunks(a->out, a->G)) most = std::max(most, pass_ranges(a->out, a->G) * n * a->RP);
   // the input gradient: a plan depends on the rows only through whole groups of 32
   for (int64_t m = 32; m < n + 32; m += 32)
     most = std::max(most, plan_values(plan_expand(a->precision == OT_BF16, false, m, a->in, a->out), m, a->in));
@@ -226,7 +244,7 @@ int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
     return p;
   };
   Work t;
-  t.n_slots = n / ot::kSlotRows + a->G + 1;
+  t.n_slots = n / kMinSlotRows + a->G + 1;       // most of either slot size
   t.perm = reinterpret_cast<int32_t*>(take(4 * n));
   t.gid = reinterpret_cast<int32_t*>(take(4 * n));
   t.off = reinterpret_cast<int32_t*>(take(4 * (a->G + 2)));
@@ -293,50 +311,87 @@ int check_values(const void* p, int align, const char* what, const char* name) {
   return OT_OK;
 }
 
+// Whether the shrink's blocks sort the ids themselves (lowrank.h).
+bool self_sorted(int64_t n, int32_t G) { return n <= ot::kSelfRows && G < ot::kSelfKeys; }
+
+int run_group(const ot_adapters* a, const int32_t* ids, int64_t n, int64_t L, const Work& w, hipStream_t st) {
+  hipLaunchKernelGGL(ot::group_rows_kernel, dim3((unsigned)(a->G + 1)), dim3(256), 0, st, ids, (int32_t)n, a->G,
+                     w.perm, w.gid, w.off, w.slots, slot_rows(L));
+  OT_LAUNCHED("group_rows_kernel");
+  return OT_OK;
+}
+
+// Sorts the rows by adapter, then the low-rank values of every row.
 template <class T>
-int run_shrink(ot::ShrinkArgs s, int64_t n, const Work& w, hipStream_t st) {
+int run_shrink(const ot_adapters* a, ot::ShrinkArgs s, const int32_t* ids, int64_t n, const Work& w, hipStream_t st) {
+  const bool self = self_sorted(n, s.G);
+  int rc;
+  if (!self && (rc = run_group(a, ids, n, s.L, w, st))) return rc;
   const int64_t splits = shrink_splits(n, s.L, s.G);
   s.k_chunk = ot::ceil_div(ot::ceil_div(s.L, splits), ot::kShrinkUnit) * ot::kShrinkUnit;
   s.splits = (int32_t)ot::ceil_div(s.L, s.k_chunk);
   s.n = n;
   s.part = w.part;
-  const dim3 grid((unsigned)w.n_slots, (unsigned)s.splits);
+  const unsigned n_slots = (unsigned)(n / slot_rows(s.L) + s.G + 1);
+  const dim3 grid(n_slots, (unsigned)s.splits);
+  const ot::SelfSort o{ids, w.perm, w.gid, w.off, w.slots, slot_rows(s.L)};
+  auto go = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    if (self) hipLaunchKernelGGL((ot::shrink_kernel<T, NT, true>), grid, dim3(ot::kShrinkThreads), 0, st, s, o);
+    else hipLaunchKernelGGL((ot::shrink_kernel<T, NT, false>), grid, dim3(ot::kShrinkThreads), 0, st, s, o);
+  };
   switch (s.RP / 16) {
-    case 1: hipLaunchKernelGGL((ot::shrink_kernel<T, 1>), grid, dim3(256), 0, st, s); break;
-    case 2: hipLaunchKernelGGL((ot::shrink_kernel<T, 2>), grid, dim3(256), 0, st, s); break;
-    case 3: hipLaunchKernelGGL((ot::shrink_kernel<T, 3>), grid, dim3(256), 0, st, s); break;
-    default: hipLaunchKernelGGL((ot::shrink_kernel<T, 4>), grid, dim3(256), 0, st, s); break;
+    case 1: go(std::integral_constant<int, 1>()); break;
+    case 2: go(std::integral_constant<int, 2>()); break;
+    case 3: go(std::integral_constant<int, 3>()); break;
+    default: go(std::integral_constant<int, 4>()); break;
   }
   OT_LAUNCHED("shrink_kernel");
   if (s.splits > 1) {
-    hipLaunchKernelGGL(ot::shrink_reduce_kernel, dim3((unsigned)w.n_slots), dim3(256), 0, st, s);
+    hipLaunchKernelGGL(ot::shrink_reduce_kernel, dim3(n_slots), dim3(256), 0, st, s);
     OT_LAUNCHED("shrink_reduce_kernel");
   }
   return OT_OK;
 }
 
-template <class T, int NT>
-int launch_outer(const ot::OuterArgs& o, int32_t G, hipStream_t st) {
-  // short rows: the wavefronts of a block share its columns and split the rows
-  const int64_t blocks = ot::ceil_div(o.L, 256) * G;
-  if (blocks < 1024)
-    hipLaunchKernelGGL((ot::outer_kernel<T, NT, true>), dim3((unsigned)ot::ceil_div(o.L, 64), (unsigned)G), dim3(256),
-                       0, st, o);
-  else
-    hipLaunchKernelGGL((ot::outer_kernel<T, NT, false>), dim3((unsigned)ot::ceil_div(o.L, 256), (unsigned)G), dim3(256),
-                       0, st, o);
-  OT_LAUNCHED("outer_kernel");
+template <class T>
+int run_pass(const ot_adapters* a, const ot::OuterArgs& o, const void* up, int64_t ldu, int64_t n, const Work& w,
+             hipStream_t st) {
+  const int chunks = pass_chunks(a->out, a->G);
+  const int64_t ranges = pass_ranges(a->out, a->G);
+  const ot::PassArgs p{o, up, ldu, w.part, n, ranges, a->RP, chunks};
+  const dim3 grid((unsigned)(ot::ceil_div(ranges, 8) * 16), (unsigned)a->G), block(ot::kPassThreads);
+  switch (a->RP / 16) {
+    case 1: hipLaunchKernelGGL((ot::pass_kernel<T, 1>), grid, block, 0, st, p); break;
+    case 2: hipLaunchKernelGGL((ot::pass_kernel<T, 2>), grid, block, 0, st, p); break;
+    case 3: hipLaunchKernelGGL((ot::pass_kernel<T, 3>), grid, block, 0, st, p); break;
+    default: hipLaunchKernelGGL((ot::pass_kernel<T, 4>), grid, block, 0, st, p); break;
+  }
+  OT_LAUNCHED("pass_kernel");
+  hipLaunchKernelGGL(ot::pass_reduce_kernel, dim3((unsigned)ot::ceil_div(n * a->RP, 16)), dim3(256), 0, st, w.part,
+                     (int32_t)ranges, n, a->RP, a->G, w.gid, o.scale, w.ts);
+  OT_LAUNCHED("pass_reduce_kernel");
   return OT_OK;
 }
 
+// Both gradients of the bank (only_down: the second alone).
 template <class T>
-int run_outer(const ot::OuterArgs& o, int32_t G, hipStream_t st) {
-  switch ((o.R + 15) / 16) {
-    case 1: return launch_outer<T, 1>(o, G, st);
-    case 2: return launch_outer<T, 2>(o, G, st);
-    case 3: return launch_outer<T, 3>(o, G, st);
-    default: return launch_outer<T, 4>(o, G, st);
+int run_outer(ot::OuterArgs up, ot::OuterArgs down, int64_t n, int32_t G, hipStream_t st, bool only_down = false) {
+  // short rows and many rows per adapter: the wavefronts of a block share its columns and split the rows
+  auto blocks = [&](ot::OuterArgs& o) {
+    o.split_rows = ot::ceil_div(o.L, 256) * G < 1024 && n > 64 * (int64_t)G;
+    return ot::ceil_div(o.L, o.split_rows ? 64 : 256);
+  };
+  const int64_t b1 = blocks(down), b0 = only_down ? 0 : blocks(up);
+  const dim3 grid((unsigned)(b0 + b1), (unsigned)G);
+  switch ((up.R + 15) / 16) {
+    case 1: hipLaunchKernelGGL((ot::outer_kernel<T, 1>), grid, dim3(256), 0, st, up, down, b0); break;
+    case 2: hipLaunchKernelGGL((ot::outer_kernel<T, 2>), grid, dim3(256), 0, st, up, down, b0); break;
+    case 3: hipLaunchKernelGGL((ot::outer_kernel<T, 3>), grid, dim3(256), 0, st, up, down, b0); break;
+    default: hipLaunchKernelGGL((ot::outer_kernel<T, 4>), grid, dim3(256), 0, st, up, down, b0); break;
   }
+  OT_LAUNCHED("outer_kernel");
+  return OT_OK;
 }
 
 // The adapted product C[row] = B A[row] (+ bias) + sum_r ts[r] mat_g[r] (ReLU or mask): the
@@ -440,13 +495,6 @@ int run_expand(const Expand& e, bool bf16, bool kmajor, float* part, hipStream_t
   return OT_OK;
 }
 
-int run_group(const ot_adapters* a, const int32_t* ids, int64_t n, const Work& w, hipStream_t st) {
-  hipLaunchKernelGGL(ot::group_rows_kernel, dim3((unsigned)(a->G + 1)), dim3(256), 0, st, ids, (int32_t)n, a->G,
-                     w.perm, w.gid, w.off, w.slots);
-  OT_LAUNCHED("group_rows_kernel");
-  return OT_OK;
-}
-
 }  // namespace
 
 extern "C" int adapters_create(ot_adapters** out, int64_t in, int64_t out_dim, int32_t rank, int32_t n_adapters,
@@ -509,10 +557,9 @@ extern "C" int adapters_forward(ot_adapters* a, const void* x, int64_t ldx, cons
   if ((rc = begin_call(a, n, st, what))) return rc;
   Work wk;
   layout(a, n, a->ws, &wk);
-  if ((rc = run_group(a, ids, n, wk, st))) return rc;
   const ot::ShrinkArgs s{x,     ldx,     down,     ldd,     a->in, 0, a->G, a->R, a->RP, 0, 0,
                          scale, wk.perm, wk.slots, nullptr, wk.ts, t, ldt};
-  rc = e == 2 ? run_shrink<uint16_t>(s, n, wk, st) : run_shrink<float>(s, n, wk, st);
+  rc = e == 2 ? run_shrink<uint16_t>(a, s, ids, n, wk, st) : run_shrink<float>(a, s, ids, n, wk, st);
   if (rc) return rc;
   const ot::AdaptRows lr{wk.perm, wk.gid, wk.off, wk.ts, up, ldu, a->G, a->R, a->RP,
                          (int32_t)(flags & OT_ADAPTERS_RELU ? 1 : 0), nullptr, 0};
@@ -556,18 +603,27 @@ extern "C" int adapters_backward(ot_adapters* a, const void* x, int64_t ldx, con
   if ((rc = begin_call(a, n, st, what))) return rc;
   Work wk;
   layout(a, n, a->ws, &wk);
-  if ((rc = run_group(a, ids, n, wk, st))) return rc;
-  if (n > 0) {
+  const ot::OuterArgs ou{dy, lddy, a->out, t, ldt, 1, scale, a->R, wk.perm, wk.off, dup, lddu, 0};
+  const ot::OuterArgs od{x, ldx, a->in, wk.ts, a->RP, 0, nullptr, a->R, wk.perm, wk.off, ddown, lddd, 0};
+  if (n == 0) {
+    if ((rc = run_group(a, ids, n, a->out, wk, st))) return rc;
+    return e == 2 ? run_outer<uint16_t>(ou, od, n, a->G, st) : run_outer<float>(ou, od, n, a->G, st);
+  }
+  const bool pass = pass_chunks(a->out, a->G) > 0;
+  if (pass) {
+    if ((rc = run_group(a, ids, n, a->out, wk, st))) return rc;
+    rc = e == 2 ? run_pass<uint16_t>(a, ou, up, ldu, n, wk, st) : run_pass<float>(a, ou, up, ldu, n, wk, st);
+    if (rc) return rc;
+    rc = e == 2 ? run_outer<uint16_t>(od, od, n, a->G, st, true) : run_outer<float>(od, od, n, a->G, st, true);
+  } else {
     const ot::ShrinkArgs s{dy,    lddy,    up,       ldu,     a->out, 0, a->G, a->R, a->RP, 0, 0,
                            scale, wk.perm, wk.slots, nullptr, wk.ts, nullptr, 0};
-    rc = e == 2 ? run_shrink<uint16_t>(s, n, wk, st) : run_shrink<float>(s, n, wk, st);
+    rc = e == 2 ? run_shrink<uint16_t>(a, s, ids, n, wk, st) : run_shrink<float>(a, s, ids, n, wk, st);
     if (rc) return rc;
+    rc = e == 2 ? run_outer<uint16_t>(ou, od, n, a->G, st) : run_outer<float>(ou, od, n, a->G, st);
   }
-  const ot::OuterArgs ou{dy, lddy, a->out, t, ldt, 1, scale, a->R, wk.perm, wk.off, dup, lddu};
-  const ot::OuterArgs od{x, ldx, a->in, wk.ts, a->RP, 0, nullptr, a->R, wk.perm, wk.off, ddown, lddd};
-  if ((rc = e == 2 ? run_outer<uint16_t>(ou, a->G, st) : run_outer<float>(ou, a->G, st))) return rc;
-  if ((rc = e == 2 ? run_outer<uint16_t>(od, a->G, st) : run_outer<float>(od, a->G, st))) return rc;
-  if (n == 0 || !dx) return OT_OK;
+  if (rc) return rc;
+  if (!dx) return OT_OK;
   const ot::AdaptRows lr{wk.perm, wk.gid, wk.off, wk.ts, down, ldd, a->G, a->R, a->RP, 0,
                          flags & OT_ADAPTERS_RELU_INPUT ? x : nullptr, ldx};
   return run_expand(Expand{dy, lddy, w, ldw, n, a->in, a->out, nullptr, dx, lddx, a->precision, lr}, e == 2, false,
