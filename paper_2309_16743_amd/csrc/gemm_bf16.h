@@ -125,10 +125,14 @@ __device__ __forceinline__ void load_target_rows(const GemmBArgs& g, int64_t m0,
     }
 }
 
-// Row numbers of the tile's sorted rows (Adapt*).
+// Row numbers and adapters of the tile's sorted rows (Adapt*).
 template <int BM>
-__device__ __forceinline__ void load_adapt_rows(const GemmBArgs& g, int64_t m0, int32_t* s_trow) {
-  for (int i = threadIdx.x; i < BM; i += blockDim.x) s_trow[i] = g.lr.perm[min(m0 + i, g.M - 1)];
+__device__ __forceinline__ void load_adapt_rows(const GemmBArgs& g, int64_t m0, int32_t* s_trow, int32_t* s_gid) {
+  for (int i = threadIdx.x; i < BM; i += blockDim.x) {
+    const int64_t m = min(m0 + i, g.M - 1);
+    s_trow[i] = g.lr.perm[m];
+    s_gid[i] = g.lr.gid[m];
+  }
 }
 
 template <int WN, EpiB EPI, int NW = 4>
@@ -771,48 +775,43 @@ __device__ __forceinline__ void adapt_offsets(int64_t (&off)[N], int wid, int la
   }
 }
 
-// What the main loop leaves out of a wavefront's sums (Adapt*, 32 x 32
-// fragments, rows mw.., columns nw..): the columns [k0, k1) past its whole k tiles, and
-// (lowrank) the rows' low-rank products.  Both come straight from memory: a
-// tile's low-rank part is rank / K of its work plus one step per adapter that
-// its rows name.  Rows of other adapters enter an adapter's product as zeros;
-// so that its infinities and NaN do not reach them, those enter as zeros too, and the
-// return value (the same for the whole wavefront) says that the epilogue has to add their
-// products to the rows they belong to (BEpi::add_odd).  The fp32 low-rank values enter as TERMS bf16 terms: two leave 2^-18 of
-// them (a bf16 result), three 2^-27 (fp32).
-template <int FM, int FN, LayB LB, int TERMS, class Acc>
-__device__ __forceinline__ bool adapt_extra(const GemmBArgs& g, Acc (&acc)[FM][FN], int64_t mw, int64_t nw,
-                                            bool lowrank, int64_t k0, int64_t k1, int lane) {
+// 8 values of column n from rows r0 + kg .. of `rows` rows of a matrix with row stride ld (kg = 0 or 8,
+// the lane's half): the wavefront-wide row r0 + e is a scalar base, the lane adds its half's 8 rows
+// and its column (below 2^31: ld and n are at most 2^26 + 8).
+__device__ __forceinline__ lr_u32x4 adapt_column(const uint16_t* p, int64_t ld, int64_t r0, int64_t rows, int64_t n,
+                                                 int kg) {
+  const uint32_t far = (uint32_t)(kg * ld + n), near = (uint32_t)n;
+  lr_u32x4 v{};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t h[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int64_t r = r0 + 2 * w + e;
+      const bool in = r + kg < rows;
+      const uint16_t* row = p + min(r, rows - 1) * ld;       // uniform
+      const uint32_t t = row[in ? far : near];
+      h[e] = in ? t : 0u;
+    }
+    v[w] = h[0] | (h[1] << 16);
+  }
+  return v;
+}
+
+// Adapt*: the columns [k0, k1) past the main loop's whole k tiles, for a wavefront's
+// 32 x 32 fragments (rows mw.., columns nw..), straight from memory.
+template <int FM, int FN, LayB LB, class Acc>
+__device__ __forceinline__ void adapt_tail(const GemmBArgs& g, Acc (&acc)[FM][FN], int64_t mw, int64_t nw, int64_t k0,
+                                           int64_t k1, int lane) {
   const int i = lane % 32, kg = 8 * (lane / 32);
   auto frag = [](lr_u32x4 v) { return __builtin_bit_cast(bf16x8, v); };
-  // 8 values of column n from rows r0 + kg .. of `rows` rows of a matrix with row stride ld: the
-  // wavefront-wide row r0 + e is a scalar base, the lane adds its half's 8 rows and its column
-  // (below 2^31: ld and n are at most 2^26 + 8)
-  auto column = [&](const uint16_t* p, int64_t ld, int64_t r0, int64_t rows, int64_t n) {
-    const uint32_t far = (uint32_t)(kg * ld + n), near = (uint32_t)n;
-    lr_u32x4 v{};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      uint32_t h[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int64_t r = r0 + 2 * w + e;
-        const bool in = r + kg < rows;
-        const uint16_t* row = p + min(r, rows - 1) * ld;     // uniform
-        const uint32_t t = row[in ? far : near];
-        h[e] = in ? t : 0u;
-      }
-      v[w] = h[0] | (h[1] << 16);
-    }
-    return v;
-  };
   for (int64_t k = k0; k < k1; k += 16) {
     bf16x8 b[FN];
 #pragma unroll
     for (int h = 0; h < FN; ++h) {
       const int64_t n = min(nw + 32 * h + i, g.N - 1);
       if constexpr (LB == LayB::KMajor) b[h] = frag(lr_load16(g.B + n * g.ldb + k + kg, k1 - k - kg));
-      else b[h] = frag(column(g.B, g.ldb, k, k1, n));
+      else b[h] = frag(adapt_column(g.B, g.ldb, k, k1, n, kg));
     }
 #pragma unroll
     for (int f = 0; f < FM; ++f) {
@@ -823,19 +822,41 @@ __device__ __forceinline__ bool adapt_extra(const GemmBArgs& g, Acc (&acc)[FM][F
       __builtin_amdgcn_sched_barrier(0);       // one fragment's operands in registers at a time
     }
   }
+}
+
+// Adapt*: the low-rank products of a wavefront's rows added to its sums, straight from
+// memory: rank / K of the tile's work plus one step per adapter that its rows name
+// (1024 x 2048 x 2048 with 32 adapters: 3 of 25 us; put before the main loop, where
+// the first k tiles' loads might have covered it, 5).  s_gid: adapters of the tile's rows from its
+// first on (LDS), wr: the wavefront's first row in the tile.  Rows of other
+// adapters enter an adapter's product as zeros; so that its infinities and NaN do not
+// reach them, those enter as zeros too, and the return value (the same for the
+// whole wavefront) says that the epilogue has to add their products to the rows they
+// belong to (BEpi::add_odd).  The fp32 low-rank values enter as TERMS bf16
+// terms: two leave 2^-18 of them (a bf16 result), three 2^-27 (fp32).
+template <int FM, int FN, int TERMS, class Acc>
+__device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM][FN], const int32_t* s_gid, int wr,
+                                              int64_t m0, int64_t nw, int lane) {
+  const int i = lane % 32, kg = 8 * (lane / 32);
+  auto frag = [](lr_u32x4 v) { return __builtin_bit_cast(bf16x8, v); };
   uint32_t odd = 0;
-  if (!lowrank) return false;
-  const int64_t me = min(mw + 32 * FM, g.M);
-  for (int64_t p = mw; p < me;) {
-    const int a = __builtin_amdgcn_readfirstlane(g.lr.gid[p]);
+  const int rows = (int)min((int64_t)(32 * FM), g.M - m0 - wr);   // rows of the wavefront that exist (may be <= 0)
+  for (int p = 0; p < rows;) {
+    const int a = __builtin_amdgcn_readfirstlane(s_gid[wr + p]);
     if (a >= g.lr.G) break;                              // rows without an adapter come last
-    const int64_t s0 = g.lr.off[a], s1 = g.lr.off[a + 1];
     const uint16_t* mat = static_cast<const uint16_t*>(g.lr.mat) + (int64_t)a * g.lr.R * g.lr.ldm;
+    uint32_t member[FM];                                 // rows of each fragment that are the adapter's
+    int next = p;
+#pragma unroll
+    for (int f = 0; f < FM; ++f) {
+      member[f] = (uint32_t)__ballot(32 * f + i < rows && s_gid[wr + 32 * f + i] == a);
+      next += __popc(member[f]);
+    }
     for (int rc = 0; rc < g.lr.RP; rc += 16) {
       bf16x8 b[FN];
 #pragma unroll
       for (int h = 0; h < FN; ++h) {
-        lr_u32x4 v = column(mat, g.lr.ldm, rc, g.lr.R, min(nw + 32 * h + i, g.N - 1));
+        lr_u32x4 v = adapt_column(mat, g.lr.ldm, rc, g.lr.R, min(nw + 32 * h + i, g.N - 1), kg);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const uint32_t lo = (v[w] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
@@ -847,11 +868,10 @@ __device__ __forceinline__ bool adapt_extra(const GemmBArgs& g, Acc (&acc)[FM][F
       }
 #pragma unroll
       for (int f = 0; f < FM; ++f) {
-        const int64_t row = mw + 32 * f + i;
-        if (max(s0, mw + 32 * f) >= min(s1, mw + 32 * f + 32)) continue;   // the same for the whole wavefront
+        if (member[f] == 0) continue;                    // the same for the whole wavefront
         float x[8];
-        const bool in = row >= s0 && row < s1;
-        const f32x4* src = reinterpret_cast<const f32x4*>(g.lr.ts + (in ? row : s0) * g.lr.RP + rc + kg);
+        const bool in = (member[f] >> i) & 1;
+        const f32x4* src = reinterpret_cast<const f32x4*>(g.lr.ts + (m0 + wr + (in ? 32 * f + i : p)) * g.lr.RP + rc + kg);
         const f32x4 lo = src[0], hi = src[1];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -868,7 +888,7 @@ __device__ __forceinline__ bool adapt_extra(const GemmBArgs& g, Acc (&acc)[FM][F
         __builtin_amdgcn_sched_barrier(0);               // one fragment's operands in registers at a time
       }
     }
-    p = s1;
+    p = next;
   }
   return __ballot(odd != 0) != 0;
 }
@@ -893,6 +913,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   __shared__ __attribute__((aligned(16))) unsigned char smem[S * STAGE_BYTES];
   __shared__ double s_red[8 + NW * WN / 2];
   __shared__ int32_t s_trow[EPI == EpiB::MseBf || is_adapt(EPI) ? BM : 1];
+  __shared__ int32_t s_gid[is_adapt(EPI) ? BM : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int wm = wid % 2, wn = wid / 2;
@@ -910,7 +931,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
-  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_gid);
 
   int64_t a_off[LA_N], b_off[LB_N];
   if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
@@ -1005,9 +1026,13 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   static_assert(S <= 4, "wait depth");
 
   bool odd = false;
-  if constexpr (is_adapt(EPI))
-    odd = adapt_extra<FM, FN, LB, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, m0 + WM * wm, n0 + WN * wn, split == 0,
-                                                                 kbeg + (int64_t)nk * BK, kend, lane);
+  if constexpr (is_adapt(EPI)) {
+    adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
+    if (split == 0) {
+      if (nk == 0) lds_barrier();        // publishes s_gid (the main loop's barriers do otherwise)
+      odd = adapt_lowrank<FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_gid, WM * wm, m0, n0 + WN * wn, lane);
+    }
+  }
 
   // Epilogue in FM / CH_F chunks of 32 CH_F rows per wave, staged through the
   // (now free) stage buffers.
@@ -1078,6 +1103,7 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   __shared__ __attribute__((aligned(16))) unsigned char smem[S * STAGE_BYTES];
   __shared__ double s_red[8 + NW * WN / 2];
   __shared__ int32_t s_trow[EPI == EpiB::MseBf || is_adapt(EPI) ? BM : 1];
+  __shared__ int32_t s_gid[is_adapt(EPI) ? BM : 1];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1095,7 +1121,7 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
-  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_gid);
 
   int64_t a_off[LA_N], b_off[LB_N];
   if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
@@ -1187,9 +1213,13 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   }
 #undef OT_WAIT_VM
   bool odd = false;
-  if constexpr (is_adapt(EPI))
-    odd = adapt_extra<FM, FN, LB, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, m0 + WM * wm, n0 + WN * wn, split == 0,
-                                                                 kbeg + (int64_t)nk * BK, kend, lane);
+  if constexpr (is_adapt(EPI)) {
+    adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
+    if (split == 0) {
+      if (nk == 0) lds_barrier();        // publishes s_gid (the main loop's barriers do otherwise)
+      odd = adapt_lowrank<FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_gid, WM * wm, m0, n0 + WN * wn, lane);
+    }
+  }
 
   float* ep = reinterpret_cast<float*>(smem) + wid * (CH_F * 32 * EP);
   BEpi<WN, EPI, NW> e(g, n0 + WN * wn);

@@ -243,51 +243,65 @@ constexpr int x3_waves(int wgn, int fm, int fn) { return (wgn == 4 || fm * fn >=
 // are meant to stay in flight.
 __device__ __forceinline__ void x3_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Low-rank products of a wavefront's rows mw.. (Adapt*), col(h): this lane's column
-// of fragment h: fp32 matrix instructions on the fp32 values, straight from memory
-// (rank / K of the tile's work).  Rows of other adapters enter as zeros, and an
+// Adapt*: low-rank products of a wavefront's rows into `sum`, col(h): this lane's column of fragment h:
+// fp32 matrix instructions on the fp32 values, straight from memory, while the first k tiles
+// are under way (rank / K of the tile's work).  s_gid: adapters of the tile's rows from m0 on (LDS),
+// wr: the wavefront's first row in the tile.  Rows of other adapters enter as zeros, and an
 // adapter's infinities and NaN too, so that they do not reach them; the return value (the
 // same for the whole wavefront) says that their products are still to be added (adapt_odd_f32).
 template <int FM, int FN, class Col>
-__device__ __forceinline__ bool adapt_lowrank_f32(const GemmArgs& g, x3_f32x16 (&acc)[FM][FN], int64_t mw, Col col) {
+__device__ __forceinline__ bool adapt_lowrank_f32(const GemmArgs& g, x3_f32x16 (&sum)[FM][FN], const int32_t* s_gid,
+                                                  int wr, int64_t m0, Col col) {
   const int lane = threadIdx.x & 63, i = lane % 32, half = lane / 32;
-  const int64_t me = min(mw + 32 * FM, g.M);
+  const int rows = (int)min((int64_t)(32 * FM), g.M - m0 - wr);   // rows of the wavefront that exist (may be <= 0)
   bool odd = false;
-  for (int64_t p = mw; p < me;) {
-    const int a = __builtin_amdgcn_readfirstlane(g.lr.gid[p]);
+  for (int p = 0; p < rows;) {
+    const int a = __builtin_amdgcn_readfirstlane(s_gid[wr + p]);
     if (a >= g.lr.G) break;                              // rows without an adapter come last
-    const int64_t s0 = g.lr.off[a], s1 = g.lr.off[a + 1];
     const float* mat = static_cast<const float*>(g.lr.mat) + (int64_t)a * g.lr.R * g.lr.ldm;
-    for (int rc = 0; rc < g.lr.RP; rc += 16) {
-      float b[FN][8];
+    uint32_t member[FM];                                 // rows of each fragment that are the adapter's
+    int next = p;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
+    for (int f = 0; f < FM; ++f) {
+      member[f] = (uint32_t)__ballot(32 * f + i < rows && s_gid[wr + 32 * f + i] == a);
+      next += __popc(member[f]);
+    }
+    for (int rc = 0; rc < g.lr.R; rc += 8) {
+      float b[FN][4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
         const int r = min(rc + 2 * q + half, g.lr.R - 1);   // ranks past R meet zeros of ts
 #pragma unroll
-        for (int h = 0; h < FN; ++h) {
-          const float v = mat[(int64_t)r * g.lr.ldm + col(h)];
-          const bool bad = !(fabsf(v) <= 3.402823466e38f);
-          odd |= bad;
-          b[h][q] = bad ? 0.f : v;
-        }
+        for (int h = 0; h < FN; ++h) b[h][q] = mat[(int64_t)r * g.lr.ldm + col(h)];
       }
+      float x[FM][4];
 #pragma unroll
       for (int f = 0; f < FM; ++f) {
-        const int64_t row = mw + 32 * f + i;
-        if (max(s0, mw + 32 * f) >= min(s1, mw + 32 * f + 32)) continue;   // the same for the whole wavefront
-        const bool in = row >= s0 && row < s1;
-        const float* ts = g.lr.ts + (in ? row : s0) * g.lr.RP + rc + half;
-        float x[8];
+        const bool in = (member[f] >> i) & 1;
+        const float* ts = g.lr.ts + (m0 + wr + (in ? 32 * f + i : p)) * g.lr.RP + rc + half;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) x[q] = ts[2 * q];
+        for (int q = 0; q < 4; ++q) x[f][q] = ts[2 * q];
+      }
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int h = 0; h < FN; ++h) {
+          const bool bad = !(fabsf(b[h][q]) <= 3.402823466e38f);
+          odd |= bad;
+          b[h][q] = bad ? 0.f : b[h][q];
+        }
+#pragma unroll
+      for (int f = 0; f < FM; ++f) {
+        if (member[f] == 0) continue;                    // the same for the whole wavefront
+        const bool in = (member[f] >> i) & 1;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int h = 0; h < FN; ++h)
-            acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x[q] : 0.f, b[h][q], acc[f][h], 0, 0, 0);
+            sum[f][h] = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x[f][q] : 0.f, b[h][q], sum[f][h], 0, 0, 0);
       }
     }
-    p = s1;
+    p = next;
   }
   return __ballot(odd) != 0;
 }
@@ -317,6 +331,7 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
   constexpr bool AD = is_adapt(EPI);
   __shared__ int32_t s_trow[EPI == Epi::Mse || AD ? BM : 1];
   __shared__ int s_hrow[AD ? BM : 1];                    // Adapt*: rows of A to sum again
+  __shared__ int32_t s_gid[AD ? BM : 1];                 // Adapt*: adapters of the rows
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -349,6 +364,7 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
   if constexpr (AD) {
     if (tid < BM) {
       s_trow[tid] = g.lr.perm[min(m0 + tid, g.M - 1)];
+      s_gid[tid] = g.lr.gid[min(m0 + tid, g.M - 1)];
       s_hrow[tid] = 0;
     }
   }
@@ -436,8 +452,14 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
     ob.store(smem + buf * BUF + OA::BYTES, big_b);
   };
   int64_t t = 0;
+  bool odd = false;
+  auto lowrank = [&](x3_f32x16 (&sum)[FM][FN]) {
+    odd = adapt_lowrank_f32<FM, FN>(g, sum, s_gid, WM * wm, m0, [&](int h) { return min(col_of(h), g.N - 1); });
+  };
   if (nk > 0) {
     load(0);
+    if constexpr (AD)
+      if (split == 0) lowrank(low);
     store(0);
     if (nk > 1) load(1);
     x3_barrier();
@@ -517,6 +539,7 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
     }
     x3_barrier();
     if constexpr (AD) {
+      if (split == 0) lowrank(acc);
       if (!(huge & 1)) {
 #pragma unroll
         for (int f = 0; f < FM; ++f)
@@ -529,9 +552,6 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
       }
     }
   }
-  bool odd = false;
-  if constexpr (AD)
-    if (split == 0) odd = adapt_lowrank_f32<FM, FN>(g, acc, m0 + WM * wm, [&](int h) { return min(col_of(h), g.N - 1); });
   if constexpr (LA == Lay::MNMajor) {
     if (do_rowsum) {                                      // uniform over the block
       float* red = reinterpret_cast<float*>(smem);        // [16][BM]
