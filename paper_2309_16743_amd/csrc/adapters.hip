@@ -142,11 +142,11 @@ int64_t shrink_splits(int64_t n, int64_t L, int32_t G) {
 
 // Block tiles (rows x columns): of gemm_bf16.h, then of gemm_f32x3.h.
 enum Tile : int {
-  kB64x64, kB64x128, kB128x128, kB128x256, kB256x256,
+  kB64x64, kB64x128, kB128x128, kB256x256,
   kX128x128, kX64x64, kX64x128, kX32x256, kX64x256
 };
-constexpr int kTileRows[] = {64, 64, 128, 128, 256, 128, 64, 64, 32, 64};
-constexpr int kTileCols[] = {64, 128, 128, 256, 256, 128, 64, 128, 256, 256};
+constexpr int kTileRows[] = {64, 64, 128, 256, 128, 64, 64, 32, 64};
+constexpr int kTileCols[] = {64, 128, 128, 256, 128, 64, 128, 256, 256};
 
 struct Plan {
   int tile;
@@ -173,13 +173,12 @@ Plan plan_expand(bool bf16, bool kmajor, int64_t M, int64_t N, int64_t K) {
   if (bf16) {
     if (kmajor) {
       if (M > 128 && tiles_of(kB256x256, M, N) >= kCUs - 16) return split_plan(kB256x256, K, 1);
-      if (M > 64 && tiles_of(kB128x256, M, N) >= kCUs - 16) return split_plan(kB128x256, K, 1);
       if (M <= 64 && tiles_of(kB64x128, M, N) >= kCUs - 16) return split_plan(kB64x128, K, 1);
       if (tiles_of(kB128x128, M, N) >= 2 * kCUs - 32) return split_plan(kB128x128, K, 1);
       if (tiles_of(kB64x128, M, N) >= 2 * kCUs - 32) return split_plan(kB64x128, K, 1);
       return split_plan(kB64x64, K, 1);
     }
-    const int big = M > 128 ? kB256x256 : M > 64 ? kB128x256 : kB64x128;
+    const int big = M > 128 ? kB256x256 : M > 64 ? kB128x128 : kB64x128;
     const int64_t t = tiles_of(big, M, N), sp = ot::ceil_div(kCUs - 16, t);
     if (K / sp >= 2048) return split_plan(big, K, sp);
     const int64_t t2 = tiles_of(kB64x128, M, N);
@@ -413,11 +412,10 @@ template <ot::LayB LB, ot::EpiB E>
 hipError_t launch_b(int tile, const ot::GemmBArgs& g, int64_t splits, hipStream_t st) {
   constexpr ot::LayB KM = ot::LayB::KMajor;
   if constexpr (LB == KM) {
-    if (tile == kB64x64) return ot::launch_gemm_bf16_pipe<64, 64, 64, 3, 3, KM, LB, E>(g, splits, st);
+    if (tile == kB64x64) return ot::launch_gemm_bf16_pipe<64, 64, 64, 4, 2, KM, LB, E>(g, splits, st);
   }
-  if (tile == kB64x128) return ot::launch_gemm_bf16_pipe<64, 128, 64, 3, 2, KM, LB, E>(g, splits, st);
+  if (tile == kB64x128) return ot::launch_gemm_bf16_pipe<64, 128, 64, 3, 4, KM, LB, E, 4>(g, splits, st);
   if (tile == kB128x128) return ot::launch_gemm_bf16_pipe<128, 128, 32, 4, 2, KM, LB, E>(g, splits, st);
-  if (tile == kB128x256) return ot::launch_gemm_bf16_pipe<128, 256, 32, 3, 2, KM, LB, E>(g, splits, st);
   return ot::launch_gemm_bf16_pp<4, KM, LB, E>(g, splits, st);
 }
 

@@ -750,6 +750,46 @@ __device__ __forceinline__ bf16x8 stage_frag(const unsigned char* st, int cpr, b
   return bf16x8{l[0], l[1], l[2], l[3], h[0], h[1], h[2], h[3]};
 }
 
+// The same operand before its data has arrived: kept as the asm statements' own
+// outputs, on which the compiler has nothing to compute, until fence() has followed the wait.
+// (As a bf16 vector it may be taken apart right after the read: a 128 x 64 tile with k tile 64
+// had its halves merged by a v_bfi ahead of the wait.)
+template <bool KMAJOR>
+struct RawFrag {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  i32x4 v;
+  i32x2 lo, hi;
+  template <int BK>
+  __device__ __forceinline__ void read(const unsigned char* st, int cpr, int base, int kk, int lane) {
+    typedef __attribute__((address_space(3))) const unsigned char lds_u8;
+    constexpr int KC = BK / 8;
+    auto lds_addr = [](const unsigned char* p) -> uint32_t { return (uint32_t)(size_t)(lds_u8*)p; };
+    if constexpr (KMAJOR) {
+      const int row = base + lane % 32;
+      const int lc = 2 * kk + lane / 32;
+      asm volatile("ds_read_b128 %0, %1" : "=v"(v) : "v"(lds_addr(st + (row * KC + (lc ^ kswz<BK>(row))) * 16)));
+    } else {
+      const int c = lane % 16, q = lane / 16;
+      const int col = base + 16 * (q & 1) + 4 * (c % 4);
+      const int r0 = 16 * kk + 8 * (q >> 1) + c / 4, r1 = r0 + 4;
+      const int ch = col / 8, half = (col / 4) & 1;
+      asm volatile("ds_read_b64_tr_b16 %0, %1"
+                   : "=v"(lo) : "v"(lds_addr(st + (r0 * cpr + (ch ^ mswz(r0))) * 16 + half * 8)));
+      asm volatile("ds_read_b64_tr_b16 %0, %1"
+                   : "=v"(hi) : "v"(lds_addr(st + (r1 * cpr + (ch ^ mswz(r1))) * 16 + half * 8)));
+    }
+  }
+  __device__ __forceinline__ void fence() {
+    if constexpr (KMAJOR) asm volatile("" : "+v"(v));
+    else asm volatile("" : "+v"(lo), "+v"(hi));
+  }
+  __device__ __forceinline__ bf16x8 get() const {
+    if constexpr (KMAJOR) return __builtin_bit_cast(bf16x8, v);
+    else return __builtin_bit_cast(bf16x8, i32x4{lo[0], lo[1], hi[0], hi[1]});
+  }
+};
+
 // Wait for the outstanding fragment reads; each fragment then passes through
 // an empty statement, so that no use of it can move above the wait.
 template <int N>
@@ -985,9 +1025,67 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   // publishes tile t + 1 comes before the MFMAs of tile t's last step, whose
   // fragments are already in registers, so stage t % S is free after it and
   // receives tile t + S.
-  bf16x8 af[FM], bfr[FN];
   for (int s = 0; s < S - 1; ++s)
     if (s < nk) issue(s, s);
+  // Small wave tiles (Adapt*) have too few MFMAs in a 16-deep step to cover its LDS reads: they read all
+  // fragments of the next k tile while the current one is multiplied, with one wait and one
+  // barrier per tile (1024 x 2048 x 2048 with 32 adapters on 64 x 64 tiles, k tile 64: 22 us, 25 by steps).
+  if constexpr (is_adapt(EPI)) {
+    typedef RawFrag<LA == LayB::KMajor> FragA;
+    typedef RawFrag<LB == LayB::KMajor> FragB;
+    FragA a0[KK][FM], a1[KK][FM];
+    FragB b0[KK][FN], b1[KK][FN];
+    auto load_tile = [&](int t, FragA (&a)[KK][FM], FragB (&b)[KK][FN]) {
+      const unsigned char* sa = smem + (t % S) * STAGE_BYTES;
+      const unsigned char* sb = sa + A_CH * 16;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f) a[kk][f].template read<BK>(sa, BM / 8, WM * wm + 32 * f, kk, lane);
+#pragma unroll
+        for (int h = 0; h < FN; ++h) b[kk][h].template read<BK>(sb, BN / 8, WN * wn + 32 * h, kk, lane);
+      }
+    };
+    auto landed = [&](FragA (&a)[KK][FM], FragB (&b)[KK][FN]) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f) a[kk][f].fence();
+#pragma unroll
+        for (int h = 0; h < FN; ++h) b[kk][h].fence();
+      }
+    };
+    auto step = [&](int kt, FragA (&a)[KK][FM], FragB (&b)[KK][FN], FragA (&an)[KK][FM], FragB (&bn)[KK][FN]) {
+      const bool more = kt + 1 < nk;
+      if (more) {
+        tile_ready(kt + 1);                            // every wave has read tile kt: its stage is free
+        if (kt + S < nk) issue(kt + S, kt % S);
+        load_tile(kt + 1, an, bn);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int h = 0; h < FN; ++h)
+            acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[kk][f].get(), b[kk][h].get(), acc[f][h], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) landed(an, bn);
+    };
+    if (nk > 0) {
+      tile_ready(0);
+      if (S - 1 < nk) issue(S - 1, S - 1);
+      load_tile(0, a0, b0);
+      landed(a0, b0);
+    }
+    for (int kt = 0; kt < nk; kt += 2) {
+      step(kt, a0, b0, a1, b1);
+      if (kt + 1 < nk) step(kt + 1, a1, b1, a0, b0);
+    }
+  } else {
+  bf16x8 af[FM], bfr[FN];
   if (nk > 0) {
     tile_ready(0);
     if (S - 1 < nk) issue(S - 1, S - 1);
@@ -1021,6 +1119,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
         for (int h = 0; h < FN; ++h) bfr[h] = bn[h];
       }
     }
+  }
   }
 #undef OT_WAIT_VM
   static_assert(S <= 4, "wait depth");
