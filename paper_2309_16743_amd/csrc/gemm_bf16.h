@@ -864,73 +864,129 @@ __device__ __forceinline__ void adapt_tail(const GemmBArgs& g, Acc (&acc)[FM][FN
   }
 }
 
-// Adapt*: the low-rank products of a wavefront's rows added to its sums, straight from
-// memory: rank / K of the tile's work plus one step per adapter that its rows name
-// (1024 x 2048 x 2048 with 32 adapters: 3 of 25 us; put before the main loop, where
-// the first k tiles' loads might have covered it, 5).  s_gid: adapters of the tile's rows from its
-// first on (LDS), wr: the wavefront's first row in the tile.  Rows of other
-// adapters enter an adapter's product as zeros; so that its infinities and NaN do not
-// reach them, those enter as zeros too, and the return value (the same for the
-// whole wavefront) says that the epilogue has to add their products to the rows they
-// belong to (BEpi::add_odd).  The fp32 low-rank values enter as TERMS bf16
-// terms: two leave 2^-18 of them (a bf16 result), three 2^-27 (fp32).
-template <int FM, int FN, int TERMS, class Acc>
-__device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM][FN], const int32_t* s_gid, int wr,
-                                              int64_t m0, int64_t nw, int lane) {
-  const int i = lane % 32, kg = 8 * (lane / 32);
+// Adapt*: what a block keeps of its tile's rows.
+template <int BM>
+struct AdaptTile {
+  int32_t gid[BM];       // their adapters
+  int32_t list[BM];      // the different adapters among them, in order
+  int32_t n;
+  int32_t odd;
+};
+
+// Adapt*: the low-rank products of the tile's rows added to the sums (acc: 32 x 32 fragments of
+// wavefront rows wr.. and columns wc.. of the tile).  The block brings the 16-rank slices of all
+// adapters that its rows name into LDS (as many as fit into `bytes` at once: one
+// latency for mostly all of them; a wavefront fetching its adapters one after the other took 190 us of
+// 1000000 x 1024 for 16 rows of 8 adapters, this XX), and each
+// wavefront multiplies those of its own rows.  Rows of other adapters enter an adapter's
+// product as zeros; so that its infinities and NaN do not reach them, those enter as zeros too, and
+// the return value (the same for the block) says that the epilogue has to add
+// their products to the rows they belong to (BEpi::add_odd).  The fp32 low-rank values enter
+// as TERMS bf16 terms: two leave 2^-18 of them (a bf16 result), three 2^-27 (fp32).
+template <int BM, int BN, int NT, int FM, int FN, int TERMS, class Acc>
+__device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM][FN], AdaptTile<BM>& t,
+                                              unsigned char* lds, int bytes, int wr, int wc, int64_t m0, int64_t n0) {
+  constexpr int PITCH = BN + 8;                          // bf16 values of a rank's row
+  const int tid = threadIdx.x, lane = tid & 63, i = lane % 32, kg = 8 * (lane / 32);
   auto frag = [](lr_u32x4 v) { return __builtin_bit_cast(bf16x8, v); };
-  uint32_t odd = 0;
-  const int rows = (int)min((int64_t)(32 * FM), g.M - m0 - wr);   // rows of the wavefront that exist (may be <= 0)
-  for (int p = 0; p < rows;) {
-    const int a = __builtin_amdgcn_readfirstlane(s_gid[wr + p]);
-    if (a >= g.lr.G) break;                              // rows without an adapter come last
-    const uint16_t* mat = static_cast<const uint16_t*>(g.lr.mat) + (int64_t)a * g.lr.R * g.lr.ldm;
-    uint32_t member[FM];                                 // rows of each fragment that are the adapter's
-    int next = p;
+  const int rows = (int)min((int64_t)BM, g.M - m0);
+  lds_barrier();                                         // the main loop's stages have been read
+  if (tid < 64) {                                        // list the adapters: each row that starts one
+    int n = 0;
+    for (int r0 = 0; r0 < rows; r0 += 64) {
+      const int r = r0 + lane;
+      const int a = r < rows ? t.gid[r] : g.lr.G;
+      const bool first = a < g.lr.G && (r == 0 || t.gid[r - 1] != a);
+      const uint64_t mask = __ballot(first);
+      if (first) t.list[n + __popcll(mask & ((1ull << lane) - 1))] = a;
+      n += __popcll(mask);
+    }
+    if (tid == 0) {
+      t.n = n;
+      t.odd = 0;
+    }
+  }
+  lds_barrier();
+  const int n_adapters = __builtin_amdgcn_readfirstlane(t.n);
+  const int batch = bytes / (16 * PITCH * 2);            // slices of 16 ranks
+  bool odd = false;
+  for (int rc = 0; rc < g.lr.RP; rc += 16) {
+    // low-rank values of this lane's rows (each row's own adapter)
+    lr_u32x4 ts[FM][TERMS];
 #pragma unroll
     for (int f = 0; f < FM; ++f) {
-      member[f] = (uint32_t)__ballot(32 * f + i < rows && s_gid[wr + 32 * f + i] == a);
-      next += __popc(member[f]);
+      const int r = wr + 32 * f + i;
+      const bool in = r < rows && t.gid[r] < g.lr.G;
+      const f32x4* src = reinterpret_cast<const f32x4*>(g.lr.ts + (m0 + (in ? r : 0)) * g.lr.RP + rc + kg);
+      f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+      if (in) {
+        lo = src[0];
+        hi = src[1];
+      }
+      const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      lr_split8<TERMS>(x, ts[f]);
     }
-    for (int rc = 0; rc < g.lr.RP; rc += 16) {
-      bf16x8 b[FN];
-#pragma unroll
-      for (int h = 0; h < FN; ++h) {
-        lr_u32x4 v = adapt_column(mat, g.lr.ldm, rc, g.lr.R, min(nw + 32 * h + i, g.N - 1), kg);
+    for (int l0 = 0; l0 < n_adapters; l0 += batch) {
+      const int nb = min(batch, n_adapters - l0);
+      if (l0 + rc > 0) lds_barrier();                    // the last batch has been read
+      for (int c = tid; c < nb * 16 * (BN / 8); c += NT) {
+        const int slice = c / (16 * (BN / 8)), r = c / (BN / 8) % 16, ch = c % (BN / 8);
+        const int64_t n = n0 + 8 * ch;
+        lr_u32x4 v = {0, 0, 0, 0};
+        if (rc + r < g.lr.R)
+          v = lr_load16(static_cast<const uint16_t*>(g.lr.mat) +
+                            ((int64_t)t.list[l0 + slice] * g.lr.R + rc + r) * g.lr.ldm + n,
+                        g.N - n);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const uint32_t lo = (v[w] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
           const uint32_t hi = (v[w] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-          odd |= lo | hi;
+          odd |= (lo | hi) != 0;
           v[w] &= ~(lo | hi);
         }
-        b[h] = frag(v);
+        *reinterpret_cast<lr_u32x4*>(lds + ((slice * 16 + r) * PITCH + 8 * ch) * 2) = v;
       }
+      lds_barrier();
+      for (int l = 0; l < nb; ++l) {
+        const int a = __builtin_amdgcn_readfirstlane(t.list[l0 + l]);
+        uint32_t member[FM];                             // rows of each fragment that are the adapter's
+        uint32_t any = 0;
 #pragma unroll
-      for (int f = 0; f < FM; ++f) {
-        if (member[f] == 0) continue;                    // the same for the whole wavefront
-        float x[8];
-        const bool in = (member[f] >> i) & 1;
-        const f32x4* src = reinterpret_cast<const f32x4*>(g.lr.ts + (m0 + wr + (in ? 32 * f + i : p)) * g.lr.RP + rc + kg);
-        const f32x4 lo = src[0], hi = src[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] = in ? lo[e] : 0.f;
-          x[4 + e] = in ? hi[e] : 0.f;
+        for (int f = 0; f < FM; ++f) {
+          const int r = wr + 32 * f + i;
+          member[f] = (uint32_t)__ballot(r < rows && t.gid[r] == a);
+          any |= member[f];
         }
-        lr_u32x4 t[TERMS];
-        lr_split8<TERMS>(x, t);
+        if (any == 0) continue;                          // the same for the whole wavefront
+        typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+        const int c = lane % 16, q = lane / 16;
+        const unsigned char* p = lds + ((l * 16 + 8 * (q >> 1) + c / 4) * PITCH + wc + 16 * (q & 1) + 4 * (c % 4)) * 2;
+        bf16x8 b[FN];
 #pragma unroll
-        for (int h = 0; h < FN; ++h)
+        for (int h = 0; h < FN; ++h) {
+          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 64 * h));
+          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 64 * h + 4 * PITCH * 2));
+          b[h] = bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        }
 #pragma unroll
-          for (int z = TERMS - 1; z >= 0; --z)
-            acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(t[z]), b[h], acc[f][h], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);               // one fragment's operands in registers at a time
+        for (int f = 0; f < FM; ++f) {
+          if (member[f] == 0) continue;                  // the same for the whole wavefront
+          const uint32_t keep = (member[f] >> i) & 1 ? 0xffffffffu : 0u;
+#pragma unroll
+          for (int z = TERMS - 1; z >= 0; --z) {
+            const lr_u32x4 x = {ts[f][z][0] & keep, ts[f][z][1] & keep, ts[f][z][2] & keep, ts[f][z][3] & keep};
+#pragma unroll
+            for (int h = 0; h < FN; ++h)
+              acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(x), b[h], acc[f][h], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);             // one fragment's operands in registers at a time
+        }
       }
     }
-    p = next;
   }
-  return __ballot(odd != 0) != 0;
+  if (odd) t.odd = 1;
+  lds_barrier();
+  return __builtin_amdgcn_readfirstlane(t.odd) != 0;
 }
 
 template <int BM, int BN, int BK, int S, int OCC, LayB LA, LayB LB, EpiB EPI, int NWN = 2>
@@ -953,7 +1009,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   __shared__ __attribute__((aligned(16))) unsigned char smem[S * STAGE_BYTES];
   __shared__ double s_red[8 + NW * WN / 2];
   __shared__ int32_t s_trow[EPI == EpiB::MseBf || is_adapt(EPI) ? BM : 1];
-  __shared__ int32_t s_gid[is_adapt(EPI) ? BM : 1];
+  __shared__ AdaptTile<is_adapt(EPI) ? BM : 1> s_at;
 
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int wm = wid % 2, wn = wid / 2;
@@ -971,7 +1027,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
-  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_gid);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at.gid);
 
   int64_t a_off[LA_N], b_off[LB_N];
   if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
@@ -1127,10 +1183,9 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   bool odd = false;
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
-    if (split == 0) {
-      if (nk == 0) lds_barrier();        // publishes s_gid (the main loop's barriers do otherwise)
-      odd = adapt_lowrank<FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_gid, WM * wm, m0, n0 + WN * wn, lane);
-    }
+    if (split == 0)
+      odd = adapt_lowrank<BM, BN, NT, FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_at, smem, S * STAGE_BYTES,
+                                                                             WM * wm, WN * wn, m0, n0);
   }
 
   // Epilogue in FM / CH_F chunks of 32 CH_F rows per wave, staged through the
@@ -1202,7 +1257,7 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   __shared__ __attribute__((aligned(16))) unsigned char smem[S * STAGE_BYTES];
   __shared__ double s_red[8 + NW * WN / 2];
   __shared__ int32_t s_trow[EPI == EpiB::MseBf || is_adapt(EPI) ? BM : 1];
-  __shared__ int32_t s_gid[is_adapt(EPI) ? BM : 1];
+  __shared__ AdaptTile<is_adapt(EPI) ? BM : 1> s_at;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1220,7 +1275,7 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
-  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_gid);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at.gid);
 
   int64_t a_off[LA_N], b_off[LB_N];
   if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
@@ -1314,10 +1369,9 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   bool odd = false;
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
-    if (split == 0) {
-      if (nk == 0) lds_barrier();        // publishes s_gid (the main loop's barriers do otherwise)
-      odd = adapt_lowrank<FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_gid, WM * wm, m0, n0 + WN * wn, lane);
-    }
+    if (split == 0)
+      odd = adapt_lowrank<BM, BN, NT, FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_at, smem, S * STAGE_BYTES,
+                                                                             WM * wm, WN * wn, m0, n0);
   }
 
   float* ep = reinterpret_cast<float*>(smem) + wid * (CH_F * 32 * EP);
