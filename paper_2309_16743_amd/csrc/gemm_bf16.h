@@ -125,13 +125,38 @@ __device__ __forceinline__ void load_target_rows(const GemmBArgs& g, int64_t m0,
     }
 }
 
-// Row numbers and adapters of the tile's sorted rows (Adapt*).
+// Adapt*: what a block keeps of its tile's rows.
 template <int BM>
-__device__ __forceinline__ void load_adapt_rows(const GemmBArgs& g, int64_t m0, int32_t* s_trow, int32_t* s_gid) {
+struct AdaptTile {
+  int32_t gid[BM];       // their adapters
+  int32_t list[BM];      // the different adapters among them, in order
+  int32_t n;
+  int32_t odd;
+};
+
+// Row numbers and adapters of the tile's sorted rows (Adapt*); the main loop's barriers publish them.
+template <int BM>
+__device__ __forceinline__ void load_adapt_rows(const GemmBArgs& g, int64_t m0, int32_t* s_trow, AdaptTile<BM>& t) {
   for (int i = threadIdx.x; i < BM; i += blockDim.x) {
     const int64_t m = min(m0 + i, g.M - 1);
     s_trow[i] = g.lr.perm[m];
-    s_gid[i] = g.lr.gid[m];
+    t.gid[i] = g.lr.gid[m];
+  }
+  if (threadIdx.x < 64) {                                // list the adapters: each row that starts one
+    int n = 0;
+#pragma unroll
+    for (int r0 = 0; r0 < BM; r0 += 64) {
+      const int64_t m = m0 + r0 + threadIdx.x;
+      const int a = m < g.M ? g.lr.gid[m] : g.lr.G;
+      const bool first = a < g.lr.G && (m == m0 || g.lr.gid[m - 1] != a);
+      const uint64_t mask = __ballot(first);
+      if (first) t.list[n + __popcll(mask & ((1ull << threadIdx.x) - 1))] = a;
+      n += __popcll(mask);
+    }
+    if (threadIdx.x == 0) {
+      t.n = n;
+      t.odd = 0;
+    }
   }
 }
 
@@ -864,20 +889,11 @@ __device__ __forceinline__ void adapt_tail(const GemmBArgs& g, Acc (&acc)[FM][FN
   }
 }
 
-// Adapt*: what a block keeps of its tile's rows.
-template <int BM>
-struct AdaptTile {
-  int32_t gid[BM];       // their adapters
-  int32_t list[BM];      // the different adapters among them, in order
-  int32_t n;
-  int32_t odd;
-};
-
 // Adapt*: the low-rank products of the tile's rows added to the sums (acc: 32 x 32 fragments of
 // wavefront rows wr.. and columns wc.. of the tile).  The block brings the 16-rank slices of all
 // adapters that its rows name into LDS (as many as fit into `bytes` at once: one
 // latency for mostly all of them; a wavefront fetching its adapters one after the other took 190 us of
-// 1000000 x 1024 for 16 rows of 8 adapters, this XX), and each
+// 1000000 x 1024 for 16 rows of 8 adapters, this 80), and each
 // wavefront multiplies those of its own rows.  Rows of other adapters enter an adapter's
 // product as zeros; so that its infinities and NaN do not reach them, those enter as zeros too, and
 // the return value (the same for the block) says that the epilogue has to add
@@ -891,22 +907,6 @@ __device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM]
   auto frag = [](lr_u32x4 v) { return __builtin_bit_cast(bf16x8, v); };
   const int rows = (int)min((int64_t)BM, g.M - m0);
   lds_barrier();                                         // the main loop's stages have been read
-  if (tid < 64) {                                        // list the adapters: each row that starts one
-    int n = 0;
-    for (int r0 = 0; r0 < rows; r0 += 64) {
-      const int r = r0 + lane;
-      const int a = r < rows ? t.gid[r] : g.lr.G;
-      const bool first = a < g.lr.G && (r == 0 || t.gid[r - 1] != a);
-      const uint64_t mask = __ballot(first);
-      if (first) t.list[n + __popcll(mask & ((1ull << lane) - 1))] = a;
-      n += __popcll(mask);
-    }
-    if (tid == 0) {
-      t.n = n;
-      t.odd = 0;
-    }
-  }
-  lds_barrier();
   const int n_adapters = __builtin_amdgcn_readfirstlane(t.n);
   const int batch = bytes / (16 * PITCH * 2);            // slices of 16 ranks
   bool odd = false;
@@ -1027,7 +1027,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
-  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at.gid);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at);
 
   int64_t a_off[LA_N], b_off[LB_N];
   if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
@@ -1275,7 +1275,7 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
   const int nk = (int)((kend - kbeg) / BK);
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
-  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at.gid);
+  if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at);
 
   int64_t a_off[LA_N], b_off[LB_N];
   if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
