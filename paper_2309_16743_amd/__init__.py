@@ -312,29 +312,48 @@ class Surrogate:
             pass
 
 
+# A small call's time is the host's, so the checks below ask each tensor for each of its properties once.
 def _matrix(t, rows: int, cols: int, dtype, what: str):
     """(pointer, leading dimension) of a rows x cols device tensor with unit column stride."""
-    if t.dtype != dtype or tuple(t.shape) != (rows, cols) or (rows > 0 and cols > 1 and t.stride(1) != 1):
+    shape, st = t.shape, t.stride()
+    if t.dtype is not dtype or len(shape) != 2 or shape[0] != rows or shape[1] != cols or (
+            rows > 0 and cols > 1 and st[1] != 1):
         raise ValueError(f"{what}: expected a {rows} x {cols} {dtype} tensor with unit column stride")
-    return _dev_ptr(t), t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor")
+    return t.data_ptr(), st[0] if rows > 1 else max(st[0], cols)
 
 
 def _bank(t, n: int, rank: int, cols: int, dtype, what: str):
     """(pointer, leading dimension) of an n x rank x cols device tensor whose rows follow each other."""
-    if t.dtype != dtype or tuple(t.shape) != (n, rank, cols) or (cols > 1 and t.stride(2) != 1):
+    shape, st = t.shape, t.stride()
+    if t.dtype is not dtype or len(shape) != 3 or shape[0] != n or shape[1] != rank or shape[2] != cols or (
+            cols > 1 and st[2] != 1):
         raise ValueError(f"{what}: expected a {n} x {rank} x {cols} {dtype} tensor with unit column stride")
-    ld = t.stride(1) if rank > 1 else t.stride(0) if n > 1 else max(t.stride(0), cols)
-    if n > 1 and t.stride(0) != rank * ld:
+    ld = st[1] if rank > 1 else st[0] if n > 1 else max(st[0], cols)
+    if n > 1 and st[0] != rank * ld:
         raise ValueError(f"{what}: the rows of successive adapters must follow each other")
-    return _dev_ptr(t), ld
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor")
+    return t.data_ptr(), ld
 
 
 def _vector(t, n: int, dtype, what: str):
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 1 or shape[0] != n or (n > 1 and t.stride()[0] != 1):
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {n} values")
-    return _dev_ptr(t)
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor")
+    return t.data_ptr()
+
+
+def _raw_stream(stream, torch):
+    """Handle of the given stream, or of the current one (without making a Stream object for it)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 class LowRankAdapters:
@@ -349,6 +368,7 @@ class LowRankAdapters:
         check("adapters_create", load().adapters_create(C.byref(h), in_dim, out_dim, rank, n_adapters, precision,
                                                         max_rows))
         self._h = h
+        self._torch, self._lib = torch, load()
         self.in_dim, self.out_dim, self.rank, self.n_adapters = in_dim, out_dim, rank, n_adapters
         self.precision = precision
         self.dtype = torch.bfloat16 if precision == OT_BF16 else torch.float32
@@ -358,7 +378,7 @@ class LowRankAdapters:
         return self._h
 
     def _common(self, x, down, up, ids, scale):
-        import torch
+        torch = self._torch
         n = x.shape[0]
         g, r = self.n_adapters, self.rank
         return (n, _matrix(x, n, self.in_dim, self.dtype, "x"),
@@ -369,23 +389,24 @@ class LowRankAdapters:
     def forward(self, x, w, down, up, ids, y, bias=None, scale=None, t=None, relu: bool = False, stream=None) -> None:
         """y = x W^T + bias + scale (x down^T) up per row's adapter (ids), in y's type
         (float32 or bfloat16); t receives x down^T for backward()."""
-        import torch
+        torch = self._torch
         n, xp, dp, up_, ip, sp = self._common(x, down, up, ids, scale)
         wp = _matrix(w, self.out_dim, self.in_dim, self.dtype, "w")
-        if y.dtype not in (torch.float32, torch.bfloat16):
+        y_type = y.dtype
+        if y_type is not torch.float32 and y_type is not torch.bfloat16:
             raise ValueError("y: expected float32 or bfloat16")
-        yp = _matrix(y, n, self.out_dim, y.dtype, "y")
+        yp = _matrix(y, n, self.out_dim, y_type, "y")
         tp = (None, 0) if t is None else _matrix(t, n, self.rank, torch.float32, "t")
-        check("adapters_forward", load().adapters_forward(
+        check("adapters_forward", self._lib.adapters_forward(
             self._h, *xp, *wp, _vector(bias, self.out_dim, torch.float32, "bias"), *dp, *up_, sp, ip, n, *yp,
-            OT_BF16 if y.dtype == torch.bfloat16 else OT_FP32, *tp, OT_ADAPTERS_RELU if relu else 0,
-            _stream_handle(stream)))
+            OT_BF16 if y_type is torch.bfloat16 else OT_FP32, *tp, OT_ADAPTERS_RELU if relu else 0,
+            _raw_stream(stream, self._torch)))
 
     def backward(self, x, w, down, up, ids, dy, t, ddown, dup, dx=None, scale=None, relu_input: bool = False,
                  stream=None) -> None:
         """Gradients of the bank into ddown, dup (fp32, whole) and, if given, of x into dx
         (relu_input: zero where x is not above 0); w and down may be None without dx."""
-        import torch
+        torch = self._torch
         n, xp, dp, up_, ip, sp = self._common(x, down, up, ids, scale)
         g, r = self.n_adapters, self.rank
         if dx is not None and (w is None or down is None):
@@ -396,9 +417,9 @@ class LowRankAdapters:
         ddp = _bank(ddown, g, r, self.in_dim, torch.float32, "ddown")
         dup_ = _bank(dup, g, r, self.out_dim, torch.float32, "dup")
         dxp = (None, 0) if dx is None else _matrix(dx, n, self.in_dim, self.dtype, "dx")
-        check("adapters_backward", load().adapters_backward(
+        check("adapters_backward", self._lib.adapters_backward(
             self._h, *xp, *wp, *dp, *up_, sp, ip, n, *dyp, *tp, *ddp, *dup_, *dxp,
-            OT_ADAPTERS_RELU_INPUT if relu_input else 0, _stream_handle(stream)))
+            OT_ADAPTERS_RELU_INPUT if relu_input else 0, _raw_stream(stream, self._torch)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -448,14 +469,15 @@ class GradientClip:
         h = C.c_void_p()
         check("clip_create", load().clip_create(C.byref(h), n, g, o, counts, types))
         self._h = h
+        self._torch, self._lib = torch, load()
 
     def norm(self, norm, stream=None) -> None:
         """The global norm into the device scalar `norm`."""
-        check("clip_norm", load().clip_norm(self._h, _scalar(norm, "norm"), _stream_handle(stream)))
+        check("clip_norm", self._lib.clip_norm(self._h, _scalar(norm, "norm", self._torch), _raw_stream(stream, self._torch)))
 
     def apply(self, max_norm: float, norm=None, stream=None) -> None:
         """Scale every tensor by min(1, max_norm / norm); the norm into `norm` (nullable)."""
-        check("clip_apply", load().clip_apply(self._h, max_norm, _scalar(norm, "norm"), _stream_handle(stream)))
+        check("clip_apply", self._lib.clip_apply(self._h, max_norm, _scalar(norm, "norm", self._torch), _raw_stream(stream, self._torch)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -469,11 +491,10 @@ class GradientClip:
             pass
 
 
-def _scalar(t, what: str):
-    import torch
+def _scalar(t, what: str, torch):
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != 1:
+    if t.dtype is not torch.float32 or t.numel() != 1:
         raise ValueError(f"{what}: expected a float32 tensor of one element")
     return _dev_ptr(t)
 
@@ -501,11 +522,12 @@ class AdamTensors:
         h = C.c_void_p()
         check("adam_create", load().adam_create(C.byref(h), n, *arrays, c, counts, lr, beta1, beta2, eps, steps))
         self._h = h
+        self._torch, self._lib = torch, load()
 
     def step(self, max_norm: float = 0.0, norm=None, stream=None) -> None:
         """One step; max_norm 0: gradients as they are.  norm (nullable): the norm before
         clipping.  A norm that is not finite takes no step."""
-        check("adam_step", load().adam_step(self._h, max_norm, _scalar(norm, "norm"), _stream_handle(stream)))
+        check("adam_step", self._lib.adam_step(self._h, max_norm, _scalar(norm, "norm", self._torch), _raw_stream(stream, self._torch)))
 
     def set_lr(self, lr: float) -> None:
         check("adam_set_lr", load().adam_set_lr(self._h, lr))

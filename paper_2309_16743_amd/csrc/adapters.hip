@@ -129,14 +129,14 @@ namespace {
 constexpr int64_t kMaxRows = 1LL << 20;
 
 // Splits of the shrink's k range (length L) for n rows: enough blocks to fill the
-// card, each with at least 16 steps per wavefront; one when the range is short,
+// card, each with at least 512 values (331 rows of 6561: 8.5 us, 15.6 with 2048); one when the range is short,
 // since the join costs a launch.  Blocks of unused slots (a large bank, few rows) are
 // not multiplied without bound.
 constexpr int64_t kShrinkBlocks = 1024;
 int64_t shrink_splits(int64_t n, int64_t L, int32_t G) {
   if (L <= 4096) return 1;
   const int64_t slots = ot::ceil_div(n, ot::kSlotRows) + std::min<int64_t>(G, n) / 2;
-  return std::max<int64_t>(1, std::min(std::min(ot::ceil_div(kShrinkBlocks, slots), L / 2048),
+  return std::max<int64_t>(1, std::min(std::min(ot::ceil_div(kShrinkBlocks, slots), L / 512),
                                        32768 / (n / ot::kSlotRows + G + 1)));
 }
 
