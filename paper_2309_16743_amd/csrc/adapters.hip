@@ -196,8 +196,12 @@ Plan plan_expand(bool bf16, bool kmajor, int64_t M, int64_t N, int64_t K) {
 // Partial sums of the plan (fp32 values; 0: not split).
 int64_t plan_values(const Plan& p, int64_t M, int64_t N) { return p.splits > 1 ? p.splits * M * ((N + 3) / 4 * 4) : 0; }
 
-// Pieces of 64 columns per wavefront in the one pass over a long dy (0: dy is short and
-// takes the two products apart).
+// The one launch over a long dy keeps a partial of every row and column range: up to
+// this many rows (131072 columns and more would fill the card's memory from 2^20 rows on anyway).
+constexpr int64_t kPassMaxRows = 4096;
+
+// Pieces of 64 columns per wavefront in that launch (0: dy is short and takes the two
+// products apart: 512 rows, 8 adapters: 65536 columns 36 + 5 us in it).
 int pass_chunks(int64_t L, int32_t G) {
   if (L < 65536) return 0;
   return (int)std::max<int64_t>(1, std::min<int64_t>(4, L / 512 * G / 1024));
@@ -227,7 +231,7 @@ int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t part_values(const ot_adapters* a, int64_t n) {
   // shrinks: splits * rows, with splits <= kShrinkBlocks / (rows / 32) + 1
   int64_t most = std::max(a->in, a->out) > 4096 ? (kShrinkBlocks * ot::kSlotRows + n) * a->RP : 0;
-  if (pass_chunks(a->out, a->G)) most = std::max(most, pass_ranges(a->out, a->G) * n * a->RP);
+  if (pass_chunks(a->out, a->G)) most = std::max(most, pass_ranges(a->out, a->G) * std::min(n, kPassMaxRows) * a->RP);
   // the input gradient: a plan depends on the rows only through whole groups of 32
   for (int64_t m = 32; m < n + 32; m += 32)
     most = std::max(most, plan_values(plan_expand(a->precision == OT_BF16, false, m, a->in, a->out), m, a->in));
@@ -607,7 +611,7 @@ extern "C" int adapters_backward(ot_adapters* a, const void* x, int64_t ldx, con
     if ((rc = run_group(a, ids, n, a->out, wk, st))) return rc;
     return e == 2 ? run_outer<uint16_t>(ou, od, n, a->G, st) : run_outer<float>(ou, od, n, a->G, st);
   }
-  const bool pass = pass_chunks(a->out, a->G) > 0;
+  const bool pass = n <= kPassMaxRows && pass_chunks(a->out, a->G) > 0;
   if (pass) {
     if ((rc = run_group(a, ids, n, a->out, wk, st))) return rc;
     rc = e == 2 ? run_pass<uint16_t>(a, ou, up, ldu, n, wk, st) : run_pass<float>(a, ou, up, ldu, n, wk, st);
