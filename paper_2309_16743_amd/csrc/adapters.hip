@@ -201,9 +201,11 @@ int64_t plan_values(const Plan& p, int64_t M, int64_t N) { return p.splits > 1 ?
 constexpr int64_t kPassMaxRows = 4096;
 
 // Pieces of 64 columns per wavefront in that launch (0: dy is short and takes the two
-// products apart: 512 rows, 8 adapters: 65536 columns 36 + 5 us in it).
+// products apart).  512 rows, 8 adapters of rank 16, all launches but the input gradient, in it and
+// apart: 8192 columns 27.2 and 26.4 us, 16384 31.0 and 32.7 (fp32 41.2 and 40.7), 65536 56 and 67
+// (fp32 98 and 110; rank 64 147 and 322), 131072 88 and 123.
 int pass_chunks(int64_t L, int32_t G) {
-  if (L < 65536) return 0;
+  if (L < 16384) return 0;
   return (int)std::max<int64_t>(1, std::min<int64_t>(4, L / 512 * G / 1024));
 }
 int64_t pass_ranges(int64_t L, int32_t G) { return ot::ceil_div(L, (int64_t)pass_chunks(L, G) * ot::kPassThreads); }
