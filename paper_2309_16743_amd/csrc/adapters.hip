@@ -168,6 +168,19 @@ Plan split_plan(int tile, int64_t K, int64_t want) {
   return p;
 }
 
+// Tile and splits by the number of blocks that each choice gives (us of the whole call, as measured with each
+// tile for all products of the kind):
+// bf16 layers: 1024 x 1000000 x 2048 on 64 x 64, 64 x 128, 128 x 128, 256 x 256 tiles 8529, 7111, 6277, 4700: the
+//   largest tile that still gives about a block per CU.  16 x 1000000 x 1024 on the same 678, 538, 638, 755: few
+//   rows stream the weights and want the blocks' loads, not their products.  1024 x 2048 x 2048 37.5, 38.9,
+//   51.9, 82.7: small tiles until every CU has blocks.
+// bf16 input gradients: 512 x 1024, k 1000000 on 256 x 256 tiles in 16, 32, 64 splits 2207, 1677, 1708, on
+//   128 x 128 2216, 2104, 2214: about a block per CU.  1024 x 2048, k 2048 on 64 x 128 tiles whole 51, in
+//   2 splits 55 (the join is a launch).
+// fp32 layers: 1024 x 10000 x 256 on 64 x 64, 64 x 128, 128 x 128 tiles 71, 66, 74.
+// fp32 input gradients (the product alone): 331 x 437, k 6561 on 128 x 128 tiles in 12, 28, 42, 60 splits 64, 41,
+//   35, 38; on 64 x 64 in 28, 60 41, 37.
+// A plan depends on the rows only through whole groups of 32 (part_values).
 Plan plan_expand(bool bf16, bool kmajor, int64_t M, int64_t N, int64_t K) {
   constexpr int64_t kCUs = 256;
   if (bf16) {
@@ -196,8 +209,8 @@ Plan plan_expand(bool bf16, bool kmajor, int64_t M, int64_t N, int64_t K) {
 // Partial sums of the plan (fp32 values; 0: not split).
 int64_t plan_values(const Plan& p, int64_t M, int64_t N) { return p.splits > 1 ? p.splits * M * ((N + 3) / 4 * 4) : 0; }
 
-// The one launch over a long dy keeps a partial of every row and column range: up to
-// this many rows (131072 columns and more would fill the card's memory from 2^20 rows on anyway).
+// The one launch over a long dy keeps a partial of every row and column range, so that its
+// workspace grows with rows times columns: it takes batches of up to this many rows.
 constexpr int64_t kPassMaxRows = 4096;
 
 // Pieces of 64 columns per wavefront in that launch (0: dy is short and takes the two

@@ -9,7 +9,13 @@
 // third launch between the two, and nothing waits on another block).
 //
 // Bound by HBM: the norm reads every gradient once, clipping reads it again
-// and writes it, Adam reads it again and reads and writes p, m, v.
+// and writes it, Adam reads it again and reads and writes p, m, v.  103.6 M fp32 elements: norm 67 us
+// (6.2 TB/s), clipping 122 (6.8 TB/s), Adam 485 (6.0 TB/s; a copy of 1 GiB reaches 5.2).  Chunks of
+// 2048 elements slow the norm to 92 us, 1024 to 113 (two dependent loads ahead of each
+// chunk's own).  96 tensors of 1.4 M elements in all: norm 3.2, clipping 4.7, Adam 11.9
+// us, each a chain of dependent loads (partials or chunk, tensor, data).
+// The squares are summed in 64 bits: the products are exact, cannot overflow or
+// underflow, and the vector units have the rate to spare.
 #include <algorithm>
 #include <cmath>
 #include <new>

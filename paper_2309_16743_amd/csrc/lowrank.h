@@ -5,7 +5,8 @@
 //   outer:  out_g[r][c] = sum over adapter g's rows of coef[p][r] src[row(p)][c]
 //
 // Both read every src value once and use each for `rank` products, so they are
-// bound by HBM (rank 16 in bf16: 16 flops a byte).  Matrix instructions keep the vector units free for addresses;
+// bound by HBM (rank 16 in bf16: 16 flops a byte), and for a batch of hidden rows by latency: 1024 rows of
+// 2048 bf16 values, rank 16, 32 adapters: shrink 8.5 us, of which 4 sort the ids, both gradients 9.5.  Matrix instructions keep the vector units free for addresses;
 // operands go from memory to registers in the lane layout of the instruction, without LDS:
 // v_mfma_f32_16x16x32_bf16: lane l supplies A[l%16][8 (l/16) + e], B[8 (l/16) + e][l%16], e = 0..7;
 // v_mfma_f32_16x16x4_f32:   lane l supplies A[l%16][l/16], B[l/16][l%16];
