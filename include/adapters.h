@@ -26,7 +26,7 @@
  * Precision OT_FP32: x, W, down, up, dy and dx are fp32.  OT_BF16: they are
  * bf16.  y is fp32 or bf16 (y_type).  bias, scale, t and the gradients ddown and
  * dup are fp32.  Sums are fp32; t and dt enter further products unrounded (as fp32
- * operands, or as a sum of bf16 terms), so a result is rounded to its type once.
+ * operands, or as a sum of three bf16 terms), so a result is rounded to its type once.
  *
  * Alignment: device pointers to x, W, down, up, dy, dx, y, ddown and dup are
  * 16-byte aligned and their leading dimensions multiples of 8 (bf16) or 4

@@ -898,11 +898,12 @@ __device__ __forceinline__ void adapt_tail(const GemmBArgs& g, Acc (&acc)[FM][FN
 // product as zeros; so that its infinities and NaN do not reach them, those enter as zeros too, and
 // the return value (the same for the block) says that the epilogue has to add
 // their products to the rows they belong to (BEpi::add_odd).  The fp32 low-rank values enter
-// as TERMS bf16 terms: two leave 2^-18 of them (a bf16 result), three 2^-27 (fp32).
-template <int BM, int BN, int NT, int FM, int FN, int TERMS, class Acc>
+// whole, as three bf16 terms of 8 significant bits each, also for a bf16 result.
+template <int BM, int BN, int NT, int FM, int FN, class Acc>
 __device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM][FN], AdaptTile<BM>& t,
                                               unsigned char* lds, int bytes, int wr, int wc, int64_t m0, int64_t n0) {
   constexpr int PITCH = BN + 8;                          // bf16 values of a rank's row
+  constexpr int TERMS = 3;
   const int tid = threadIdx.x, lane = tid & 63, i = lane % 32, kg = 8 * (lane / 32);
   auto frag = [](lr_u32x4 v) { return __builtin_bit_cast(bf16x8, v); };
   const int rows = (int)min((int64_t)BM, g.M - m0);
@@ -924,7 +925,7 @@ __device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM]
         hi = src[1];
       }
       const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      lr_split8<TERMS>(x, ts[f]);
+      lr_split8(x, ts[f]);
     }
     for (int l0 = 0; l0 < n_adapters; l0 += batch) {
       const int nb = min(batch, n_adapters - l0);
@@ -1184,8 +1185,7 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
     if (split == 0)
-      odd = adapt_lowrank<BM, BN, NT, FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_at, smem, S * STAGE_BYTES,
-                                                                             WM * wm, WN * wn, m0, n0);
+      odd = adapt_lowrank<BM, BN, NT, FM, FN>(g, acc, s_at, smem, S * STAGE_BYTES, WM * wm, WN * wn, m0, n0);
   }
 
   // Epilogue in FM / CH_F chunks of 32 CH_F rows per wave, staged through the
@@ -1370,8 +1370,7 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
     if (split == 0)
-      odd = adapt_lowrank<BM, BN, NT, FM, FN, EPI == EpiB::AdaptF32 ? 3 : 2>(g, acc, s_at, smem, S * STAGE_BYTES,
-                                                                             WM * wm, WN * wn, m0, n0);
+      odd = adapt_lowrank<BM, BN, NT, FM, FN>(g, acc, s_at, smem, S * STAGE_BYTES, WM * wm, WN * wn, m0, n0);
   }
 
   float* ep = reinterpret_cast<float*>(smem) + wid * (CH_F * 32 * EP);

@@ -360,7 +360,7 @@ __device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, i
           x[e] = p < pe ? coef(p, row[e], q) : 0.f;
         }
         lr_u32x4 t[TERMS];
-        lr_split8<TERMS>(x, t);
+        lr_split8(x, t);
 #pragma unroll
         for (int z = TERMS - 1; z >= 0; --z)
 #pragma unroll
@@ -483,7 +483,7 @@ __device__ __forceinline__ void pass_outer(const PassArgs& a, int64_t range, int
       }
       if constexpr (BF) {
         lr_u32x4 t[3];
-        lr_split8<3>(x, t);
+        lr_split8(x, t);
 #pragma unroll
         for (int z = 0; z < 3; ++z) sh.coef[s][q][z][l] = t[z];
       } else {

@@ -53,11 +53,11 @@ __device__ __forceinline__ lr_u32x4 lr_load16(const T* p, int64_t valid) {
   return q;
 }
 
-// x as a sum of TERMS bf16 values, packed in pairs: t[q] holds term q of 8 values.
-// Two terms leave 2^-18 of x, three 2^-27.  Infinities and NaN: the first term
+// x as a sum of three bf16 values, packed in pairs: t[q] holds term q of 8 values.
+// Three terms hold the 24 bits of x (two would leave 2^-18 of it).  Infinities and NaN: the first term
 // holds them, later ones are zero (inf - inf would be NaN).
-template <int TERMS>
-__device__ __forceinline__ void lr_split8(const float (&x)[8], lr_u32x4 (&t)[TERMS]) {
+__device__ __forceinline__ void lr_split8(const float (&x)[8], lr_u32x4 (&t)[3]) {
+  constexpr int TERMS = 3;
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   float rest[8];
 #pragma unroll
