@@ -842,10 +842,10 @@ __device__ __forceinline__ void adapt_offsets(int64_t (&off)[N], int wid, int la
 
 // 8 values of column n from rows r0 + kg .. of `rows` rows of a matrix with row stride ld (kg = 0 or 8,
 // the lane's half): the wavefront-wide row r0 + e is a scalar base, the lane adds its half's 8 rows
-// and its column (below 2^31: ld and n are at most 2^26 + 8).
+// and its column (in 64 bits: a caller's ld may be anything, a slice of a wide array's rows too).
 __device__ __forceinline__ lr_u32x4 adapt_column(const uint16_t* p, int64_t ld, int64_t r0, int64_t rows, int64_t n,
                                                  int kg) {
-  const uint32_t far = (uint32_t)(kg * ld + n), near = (uint32_t)n;
+  const int64_t far = kg * ld + n;
   lr_u32x4 v{};
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -855,7 +855,7 @@ __device__ __forceinline__ lr_u32x4 adapt_column(const uint16_t* p, int64_t ld, 
       const int64_t r = r0 + 2 * w + e;
       const bool in = r + kg < rows;
       const uint16_t* row = p + min(r, rows - 1) * ld;       // uniform
-      const uint32_t t = row[in ? far : near];
+      const uint32_t t = row[in ? far : n];
       h[e] = in ? t : 0u;
     }
     v[w] = h[0] | (h[1] << 16);
