@@ -17,6 +17,7 @@ python -m paper_2309_16743_amd.finetune runs a small demonstration.
 """
 from __future__ import annotations
 
+import contextlib
 import math
 from typing import Optional
 
@@ -39,7 +40,14 @@ class AdapterTrainer:
     the adapters in bf16 (the first layer, fed by raw temperatures, stays fp32 as in
     the surrogate); master adapters, gradients and Adam are fp32.  alpha: the adapters'
     scale is alpha / rank.  max_norm: bound of the gradients' global norm (0: none).
-    up starts at zero, so the adapted surrogate starts as the trained one."""
+    up starts at zero, so the adapted surrogate starts as the trained one.
+
+    A call runs on the stream current when it is made, behind the trainer's call before it
+    whichever stream that ran on.  With a stream given here every call runs on that one,
+    behind what the caller's current stream holds, and the current stream waits for it in
+    turn, so inputs and results belong to the current stream in both cases.  A call under
+    capture waits for nothing but its own stream, or forks from it and joins it again; the
+    order of replays among other calls is the caller's."""
 
     def __init__(self, surrogate: Surrogate, n_ensembles: int, rank: int = 8, batch: int = 1024,
                  precision: int = OT_FP32, lr: float = 1e-3, alpha: Optional[float] = None, max_norm: float = 1.0,
@@ -47,10 +55,12 @@ class AdapterTrainer:
         dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
         self.widths, self.batch, self.rank, self.n_ensembles = surrogate.widths, batch, rank, n_ensembles
         self.max_norm = max_norm
-        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self.stream = stream
+        # where the buffers below are allocated, and where the last call ran
+        self._home = self._last = stream if stream is not None else torch.cuda.current_stream()
         op = torch.bfloat16 if precision == OT_BF16 else torch.float32
         layers = len(self.widths) - 1
-        with torch.cuda.stream(self.stream):
+        with torch.cuda.stream(self._home):
             gen = torch.Generator(device=dev)
             gen.manual_seed(seed)
             self.scale = torch.full((n_ensembles,), (float(rank) if alpha is None else alpha) / rank, device=dev)
@@ -94,6 +104,27 @@ class AdapterTrainer:
             self.adam = AdamTensors(params, grads, self.m, self.v, copies=copies, lr=lr)
             self.norm = torch.zeros(1, device=dev)
             self.loss = torch.zeros(1, device=dev)
+        if stream is not None:
+            torch.cuda.current_stream().wait_stream(stream)
+
+    @contextlib.contextmanager
+    def _ordered(self):
+        """The call's stream as the current one, in order with the caller's stream and the call before."""
+        here = torch.cuda.current_stream()
+        if self.stream is not None:
+            if self.stream == here:
+                yield
+                return
+            self.stream.wait_stream(here)
+            with torch.cuda.stream(self.stream):
+                yield
+            here.wait_stream(self.stream)
+            return
+        if not torch.cuda.is_current_stream_capturing():
+            if self._last != here:
+                here.wait_stream(self._last)
+            self._last = here
+        yield
 
     @property
     def n_layers(self) -> int:
@@ -108,21 +139,21 @@ class AdapterTrainer:
             last = l + 1 == self.n_layers
             y = out if last and out is not None else self.acts[l][:n]
             bank.forward(a, self.w[l], self.down[l], self.up[l], ids, y, bias=self.bias[l], scale=self.scale,
-                         t=self.t[l][:n] if save else None, relu=not last, stream=self.stream)
+                         t=self.t[l][:n] if save else None, relu=not last)
             a = y
         return a
 
     def predict(self, x, ids, y) -> None:
         """y (fp32 or bf16, rows padded to whole 16-byte pieces) of up to `batch` rows x, each with its
         ensemble's adapters (an id outside the bank: the surrogate as it was)."""
-        with torch.cuda.stream(self.stream):
+        with self._ordered():
             self._forward(x, ids, out=y)
 
     def train_step(self, x, u, ids) -> None:
         """One step on rows x -> u of ensembles ids: mean squared error, gradients of every adapter, clipping,
         Adam.  self.loss and self.norm receive the loss and the gradients' norm before clipping."""
         n = x.shape[0]
-        with torch.cuda.stream(self.stream):
+        with self._ordered():
             y = self._forward(x, ids, save=True)
             r = y - u
             self.loss.copy_((r * r).mean())
@@ -133,19 +164,27 @@ class AdapterTrainer:
                 inp = x if l == 0 else self.acts[l - 1][:n]
                 dx = None if l == 0 else self.dx[l][:n]
                 self.banks[l].backward(inp, self.w[l], self.down[l], self.up[l], ids, dy, self.t[l][:n],
-                                       self.ddown[l], self.dup[l], dx=dx, scale=self.scale, relu_input=l > 0,
-                                       stream=self.stream)
+                                       self.ddown[l], self.dup[l], dx=dx, scale=self.scale, relu_input=l > 0)
                 if l > 0:
                     dy = dx
                     if l == 1 and dx.dtype != self.grads_in[0].dtype:     # the first layer computes in fp32
                         dy = self.grads_in[0][:n]
                         dy.copy_(dx)
-            self.adam.step(self.max_norm, self.norm, stream=self.stream)
+            self.adam.step(self.max_norm, self.norm)
 
     def close(self) -> None:
+        if self._last != self._home:           # the buffers go back to the allocations of the stream they are from
+            self._home.wait_stream(self._last)
+            self._last = self._home
         for b in self.banks:
             b.close()
         self.adam.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def main() -> None:
