@@ -281,6 +281,29 @@ __global__ __launch_bounds__(256) void shrink_reduce_kernel(ShrinkArgs a) {
 }
 
 // ------------------------------------------------------------------ outer
+// Pairs of bf16 values with infinities and NaN as zeros.
+__device__ __forceinline__ lr_u32x4 lr_finite(lr_u32x4 v) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t bad = ((v[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // exponents of all ones carry out
+    v[w] &= ~((bad >> 15) * 0xffffu);
+  }
+  return v;
+}
+
+// Whether any sum of the wavefront is NaN (the same for all its lanes).
+template <int NT>
+__device__ __forceinline__ bool lr_any_nan(const f32x4 (&acc)[NT][4]) {
+  bool nan = false;
+#pragma unroll
+  for (int q = 0; q < NT; ++q)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) nan |= acc[q][j][r] != acc[q][j][r];
+  return __ballot(nan) != 0;
+}
+
 struct OuterArgs {
   const void* src;        // rows of L values
   int64_t lds;
@@ -301,22 +324,20 @@ struct OuterArgs {
 // that it reads 8 or 16 bytes of a row and writes 16 bytes of an output row; column
 // q of the four is one matrix product.  In bf16 the rows' coefficients enter as
 // three bf16 terms (they are fp32), 32 rows to a step; in fp32 4 rows to a product.
+// An infinite src times a coefficient's later terms (zero, or of the other sign) would
+// be a NaN that the product itself is not: sums that end as NaN are formed again with
+// such values against the first term alone, which also gives the NaN that are right.
 //
-// split_rows false: the block's wavefronts take 64 columns each (long rows: enough
-// blocks).  true: they take the same 64 columns and every fourth step of 32
-// rows, and join in LDS (short rows: four times the wavefronts).
-template <class T, int NT, bool ROWSPLIT>
-__device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, int g, float (*red)[16 * NT][68]) {
+// Sums of a wavefront's 64 columns from c0 over the adapter's sorted rows p0, p0 + 1 .. p0 + 31, then from p0 + STRIDE
+// on.  AGAIN: infinities and NaN of src meet the first term only.
+template <class T, int NT, int STRIDE, bool AGAIN>
+__device__ __forceinline__ void outer_sums(const OuterArgs& a, int64_t c0, int g, int p0, f32x4 (&acc)[NT][4]) {
   constexpr int TERMS = 3;
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int64_t c0 = (block * (ROWSPLIT ? 1 : 4) + (ROWSPLIT ? 0 : wid)) * 64;
-  if (!ROWSPLIT && c0 >= a.L) return;             // no barriers follow
-  const int pb = a.off[g], pe = a.off[g + 1];
-  const int i = lane % 16, kg = lane / 16;
+  const int lane = threadIdx.x & 63, i = lane % 16, kg = lane / 16;
+  const int pe = a.off[g + 1];
   const int64_t c = c0 + 4 * i;
   const int64_t cl = c < a.L ? c : 0;             // lanes past the row read its start; they store nothing
   const float sc = a.by_row && a.scale ? a.scale[g] : 1.f;
-  f32x4 acc[NT][4];
 #pragma unroll
   for (int q = 0; q < NT; ++q)
 #pragma unroll
@@ -326,7 +347,7 @@ __device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, i
     const int r = 16 * q + i;
     return r < a.R ? sc * a.coef[(a.by_row ? row : (int64_t)p) * a.ldc + r] : 0.f;
   };
-  for (int p0 = pb + (ROWSPLIT ? 32 * wid : 0); p0 < pe; p0 += ROWSPLIT ? 128 : 32) {
+  for (; p0 < pe; p0 += STRIDE) {
     int64_t row[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -364,7 +385,8 @@ __device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, i
 #pragma unroll
         for (int z = TERMS - 1; z >= 0; --z)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[q][j] = lr_mfma<uint16_t>(t[z], b[j], acc[q][j]);
+          for (int j = 0; j < 4; ++j)
+            acc[q][j] = lr_mfma<uint16_t>(t[z], AGAIN && z > 0 ? lr_finite(b[j]) : b[j], acc[q][j]);
       }
     } else {
       f32x4 v[8];
@@ -385,7 +407,43 @@ __device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, i
       }
     }
   }
-  // element r of acc[q][j]: rank 16 q + 4 kg + r, column c + j
+}
+
+// Element r of acc[q][j] is rank 16 q + 4 (l/16) + r, column c0 + 4 (l%16) + j.
+template <int NT>
+__device__ __forceinline__ void outer_store(const OuterArgs& a, int64_t c0, int g, const f32x4 (&acc)[NT][4]) {
+  const int lane = threadIdx.x & 63, kg = lane / 16;
+  const int64_t c = c0 + 4 * (lane % 16);
+#pragma unroll
+  for (int q = 0; q < NT; ++q)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int rank = 16 * q + 4 * kg + r;
+      if (rank >= a.R || c >= a.L) continue;
+      float* o = a.out + ((int64_t)g * a.R + rank) * a.ldo + c;
+      if (c + 4 <= a.L) {
+        *reinterpret_cast<f32x4*>(o) = f32x4{acc[q][0][r], acc[q][1][r], acc[q][2][r], acc[q][3][r]};
+      } else {
+        for (int j = 0; c + j < a.L; ++j) o[j] = j == 0 ? acc[q][0][r] : j == 1 ? acc[q][1][r] : acc[q][2][r];
+      }
+    }
+}
+
+// split_rows false: the block's wavefronts take 64 columns each (long rows: enough
+// blocks).  true: they take the same 64 columns and every fourth step of 32
+// rows, and join in LDS (short rows: four times the wavefronts).
+template <class T, int NT, bool ROWSPLIT>
+__device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, int g, float (*red)[16 * NT][68]) {
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, i = lane % 16, kg = lane / 16;
+  const int64_t c0 = (block * (ROWSPLIT ? 1 : 4) + (ROWSPLIT ? 0 : wid)) * 64;
+  if (!ROWSPLIT && c0 >= a.L) return;             // no barriers follow
+  constexpr int STRIDE = ROWSPLIT ? 128 : 32;
+  const int p0 = a.off[g] + (ROWSPLIT ? 32 * wid : 0);
+  f32x4 acc[NT][4];
+  outer_sums<T, NT, STRIDE, false>(a, c0, g, p0, acc);
+  if constexpr (sizeof(T) == 2) {
+    if (lr_any_nan(acc)) outer_sums<T, NT, STRIDE, true>(a, c0, g, p0, acc);
+  }
   if constexpr (ROWSPLIT) {
     if (wid > 0) {
 #pragma unroll
@@ -407,19 +465,7 @@ __device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, i
           acc[q][j][r] = ((acc[q][j][r] + red[0][rr][cc]) + red[1][rr][cc]) + red[2][rr][cc];
         }
   }
-#pragma unroll
-  for (int q = 0; q < NT; ++q)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int rank = 16 * q + 4 * kg + r;
-      if (rank >= a.R || c >= a.L) continue;
-      float* o = a.out + ((int64_t)g * a.R + rank) * a.ldo + c;
-      if (c + 4 <= a.L) {
-        *reinterpret_cast<f32x4*>(o) = f32x4{acc[q][0][r], acc[q][1][r], acc[q][2][r], acc[q][3][r]};
-      } else {
-        for (int j = 0; c + j < a.L; ++j) o[j] = j == 0 ? acc[q][0][r] : j == 1 ? acc[q][1][r] : acc[q][2][r];
-      }
-    }
+  outer_store<NT>(a, c0, g, acc);
 }
 
 // Both low-rank products of a long dy in one launch (its rows are the largest array of a
@@ -467,6 +513,7 @@ __device__ __forceinline__ void pass_outer(const PassArgs& a, int64_t range, int
   const int64_t w0 = range * a.chunks * NW * 64 + wid * 64;
   const float sc = a.o.scale ? a.o.scale[g] : 1.f;
   const T* const src = static_cast<const T*>(a.o.src);
+  bool nan = false;                                // the same for the wavefront
   for (int p0 = pb; p0 < pe || p0 == pb; p0 += kPassRows) {    // also once for an adapter without rows
     const int cnt = min(kPassRows, pe - p0);
     __syncthreads();                               // the last round's coefficients have been read
@@ -597,11 +644,21 @@ __device__ __forceinline__ void pass_outer(const PassArgs& a, int64_t range, int
           if (ms == 0) clear();
           multiply(ms, v[u]);
           if (++ms == steps) {
+            if constexpr (BF) nan |= lr_any_nan(acc);
             store(mch);
             ms = 0;
             ++mch;
           }
         }
+      }
+    }
+  }
+  if constexpr (BF) {
+    if (nan) {                                     // as in outer_block: rare, so each piece again, over all its rows
+      f32x4 acc[NT][4];
+      for (int64_t c0 = w0; c0 < min(a.o.L, w0 + NW * 64 * a.chunks); c0 += NW * 64) {
+        outer_sums<T, NT, 32, true>(a.o, c0, g, pb, acc);
+        outer_store<NT>(a.o, c0, g, acc);
       }
     }
   }

@@ -61,3 +61,71 @@ def test_input_gradient_takes_low_rank_values_whole(n, n_in, n_out):
     bank.backward(x, w, down, up, ids, dy, t, ddown, dup, dx=dx)
     assert bool((dx == 2.0 ** -20).all())
     bank.close()
+
+
+def special(gen, n, cols, dtype):
+    """Values in (-1, 1) of which some are zero, and in rows 1, 4, 7, .. some infinities of either sign and NaN."""
+    a = zeros(n, cols, dtype=dtype)
+    a.uniform_(-1, 1, generator=gen)
+    at = torch.rand(n, cols, generator=gen, device=DEV)
+    a[at < 0.1] = 0.0
+    odd = (torch.arange(n, device=DEV) % 3 == 1)[:, None]
+    for lo, v in ((0.90, float("inf")), (0.93, float("-inf")), (0.96, float("nan"))):
+        a[odd & (at >= lo) & (at < lo + 0.01)] = v
+    return a
+
+
+def outer(coef, src, ids, g):
+    """sum over each adapter's rows of coef^T src in 64 bits, term by term (a matrix product may skip zeros)."""
+    out = torch.zeros(g, coef.shape[1], src.shape[1], dtype=torch.float64, device=DEV)
+    for i, k in enumerate(ids.tolist()):
+        if 0 <= k < g:
+            out[k] += coef[i].double()[:, None] * src[i].double()[None, :]
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("n,n_in,n_out,r,g", [(40, 33, 70, 3, 5), (200, 70, 130, 5, 1), (30, 40, 20_001, 17, 2),
+                                              (300, 40, 17_000, 4, 2), (70, 20, 131_000, 40, 1)])
+def test_infinities_in_the_gradients_of_a_bank(n, n_in, n_out, r, g, dtype):
+    """dup where dy holds infinities and ddown where x does: infinite, NaN and finite where the formula's terms
+    are, and the finite values within the bound of their sums (4 sqrt(n) of 2^-24 of the sum of absolute values)."""
+    from paper_2309_16743_amd import OT_BF16, OT_FP32, LowRankAdapters
+    print(f"infinities {n} {n_in} {n_out} {r} {g} {dtype}", flush=True)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(n)
+    bank = LowRankAdapters(n_in, n_out, r, g, precision=OT_BF16 if dtype == BF else OT_FP32, max_rows=n)
+    ids = torch.randint(-1 if g > 1 else 0, g, (n,), generator=gen, device=DEV).to(torch.int32)
+    t = torch.empty(n, r, device=DEV).uniform_(-1, 1, generator=gen)
+    t[::4, ::2] = 0.0
+    t[2::4, ::2] = 0.5                                             # one term holds it, the others are zero
+    up = zeros(g, r, n_out, dtype=dtype)
+    up.uniform_(-1, 1, generator=gen)
+    ddown, dup = (zeros(g, r, c, dtype=torch.float32) for c in (n_in, n_out))
+
+    def check(got, coef, src):
+        want, size = outer(coef, src, ids, g), outer(coef.abs(), src.abs(), ids, g)
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        inf = torch.isinf(want)
+        assert torch.equal(torch.isinf(got), inf) and torch.equal(got[inf].double(), want[inf])
+        fine = torch.isfinite(want)
+        assert bool(((got.double() - want).abs()[fine] <= (4 * n ** 0.5 + 16) * 2.0 ** -24 * size[fine] + 1e-30).all())
+        assert bool(inf.any()) and bool(fine.any())
+
+    x = zeros(n, n_in, dtype=dtype)
+    x.uniform_(0, 1, generator=gen)
+    dy = special(gen, n, n_out, dtype)
+    bank.backward(x, None, None, up, ids, dy, t, ddown, dup)
+    check(dup, t, dy)
+    # dt of few bits, so that the 64-bit sums start from the kernel's own: dy and up of small whole numbers
+    x = special(gen, n, n_in, dtype)
+    dy, up = zeros(n, n_out, dtype=dtype), zeros(g, r, n_out, dtype=dtype)
+    dy[:, :8] = torch.randint(-2, 3, (n, 8), generator=gen, device=DEV).to(dtype)
+    up[..., :8] = torch.randint(-2, 3, (g, r, 8), generator=gen, device=DEV).to(dtype)
+    bank.backward(x, None, None, up, ids, dy, t, ddown, dup)
+    dt = torch.zeros(n, r, device=DEV)
+    for i, k in enumerate(ids.tolist()):
+        if k >= 0:
+            dt[i] = (up[k].float() * dy[i].float()).sum(1)
+    check(ddown, dt, x)
+    bank.close()
