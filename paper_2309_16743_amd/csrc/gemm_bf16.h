@@ -170,7 +170,7 @@ struct BEpi {
   bool cfull;
   const int32_t* s_trow = nullptr;   // MseBf with target_rows: row indices of the tile (LDS), row tile_m0 first
   int64_t tile_m0 = 0;
-  bool odd = false;                  // Adapt*: values that are not finite were left out of the low-rank product
+  bool odd = false;                  // Adapt*: values that are not finite were left out of the low-rank products
   __device__ __forceinline__ int64_t trow(const GemmBArgs& g, int64_t m) const {
     return g.target_rows ? (int64_t)s_trow[m - tile_m0] : m;
   }
@@ -286,15 +286,16 @@ struct BEpi {
     }
   }
 
-  // Adapt*: the products with values of the row's own adapter that are not finite.
+  // Adapt*: the products of the row's own adapter of which a factor is not finite (a low-rank value past
+  // bf16's range included: its first term would be infinite).
   __device__ __forceinline__ void add_odd(const GemmBArgs& g, int64_t m, float (&v)[4]) const {
     const int a = g.lr.gid[m];
     if (a >= g.lr.G) return;
     for (int r = 0; r < g.lr.R; ++r) {
       const uint16_t* p = static_cast<const uint16_t*>(g.lr.mat) + ((int64_t)a * g.lr.R + r) * g.lr.ldm + col;
       for (int c = 0; c < 4; ++c) {
-        const float x = col + c < g.N ? bf2f(p[c]) : 0.f;
-        if (!(fabsf(x) <= 3.402823466e38f)) v[c] = fmaf(g.lr.ts[m * g.lr.RP + r], x, v[c]);
+        const float x = col + c < g.N ? bf2f(p[c]) : 0.f, t = g.lr.ts[m * g.lr.RP + r];
+        if (!(fabsf(x) <= kBf16Max && fabsf(t) <= kBf16Max)) v[c] = fmaf(t, x, v[c]);
       }
     }
   }
@@ -895,7 +896,8 @@ __device__ __forceinline__ void adapt_tail(const GemmBArgs& g, Acc (&acc)[FM][FN
 // latency for mostly all of them; a wavefront fetching its adapters one after the other took 190 us of
 // 1000000 x 1024 for 16 rows of 8 adapters, this 80), and each
 // wavefront multiplies those of its own rows.  Rows of other adapters enter an adapter's
-// product as zeros; so that its infinities and NaN do not reach them, those enter as zeros too, and
+// product as zeros; so that its infinities and NaN do not reach them, those enter as zeros too, as do
+// a row's low-rank values that are not finite (times such a zero they would be NaN), and
 // the return value (the same for the block) says that the epilogue has to add
 // their products to the rows they belong to (BEpi::add_odd).  The fp32 low-rank values enter
 // whole, as three bf16 terms of 8 significant bits each, also for a bf16 result.
@@ -924,7 +926,13 @@ __device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM]
         lo = src[0];
         hi = src[1];
       }
-      const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool bad = !(fabsf(x[e]) <= kBf16Max);
+        odd |= bad;
+        x[e] = bad ? 0.f : x[e];
+      }
       lr_split8(x, ts[f]);
     }
     for (int l0 = 0; l0 < n_adapters; l0 += batch) {

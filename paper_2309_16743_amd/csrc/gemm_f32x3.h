@@ -247,7 +247,8 @@ __device__ __forceinline__ void x3_barrier() { asm volatile("s_waitcnt lgkmcnt(0
 // fp32 matrix instructions on the fp32 values, straight from memory, while the first k tiles
 // are under way (rank / K of the tile's work).  s_gid: adapters of the tile's rows from m0 on (LDS),
 // wr: the wavefront's first row in the tile.  Rows of other adapters enter as zeros, and an
-// adapter's infinities and NaN too, so that they do not reach them; the return value (the
+// adapter's infinities and NaN too, so that they do not reach them, as do a row's low-rank values that are
+// not finite (times such a zero they would be NaN); the return value (the
 // same for the whole wavefront) says that their products are still to be added (adapt_odd_f32).
 template <int FM, int FN, class Col>
 __device__ __forceinline__ bool adapt_lowrank_f32(const GemmArgs& g, x3_f32x16 (&sum)[FM][FN], const int32_t* s_gid,
@@ -295,10 +296,13 @@ __device__ __forceinline__ bool adapt_lowrank_f32(const GemmArgs& g, x3_f32x16 (
         if (member[f] == 0) continue;                    // the same for the whole wavefront
         const bool in = (member[f] >> i) & 1;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 4; ++q) {
+          const bool bad = in && !(fabsf(x[f][q]) <= 3.402823466e38f);
+          odd |= bad;
+          const float v = in && !bad ? x[f][q] : 0.f;
 #pragma unroll
-          for (int h = 0; h < FN; ++h)
-            sum[f][h] = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x[f][q] : 0.f, b[h][q], sum[f][h], 0, 0, 0);
+          for (int h = 0; h < FN; ++h) sum[f][h] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, b[h][q], sum[f][h], 0, 0, 0);
+        }
       }
     }
     p = next;
@@ -306,13 +310,14 @@ __device__ __forceinline__ bool adapt_lowrank_f32(const GemmArgs& g, x3_f32x16 (
   return __ballot(odd) != 0;
 }
 
-// x with the products of sorted row m's own adapter whose value is not finite.
+// x with the products of sorted row m's own adapter of which a factor is not finite.
 __device__ __forceinline__ float adapt_odd_f32(const GemmArgs& g, int64_t m, int64_t n, float x) {
   const int a = g.lr.gid[m];
   if (a >= g.lr.G) return x;
   for (int r = 0; r < g.lr.R; ++r) {
     const float v = static_cast<const float*>(g.lr.mat)[((int64_t)a * g.lr.R + r) * g.lr.ldm + n];
-    if (!(fabsf(v) <= 3.402823466e38f)) x = fmaf(g.lr.ts[m * g.lr.RP + r], v, x);
+    const float t = g.lr.ts[m * g.lr.RP + r];
+    if (!(fabsf(v) <= 3.402823466e38f && fabsf(t) <= 3.402823466e38f)) x = fmaf(t, v, x);
   }
   return x;
 }

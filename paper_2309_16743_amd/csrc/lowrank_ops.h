@@ -21,6 +21,8 @@ struct AdaptRows {
   int64_t ldmask;
 };
 
+constexpr float kBf16Max = 3.3895313892515355e38f;   // larger finite fp32 values may round to infinity in bf16
+
 typedef __bf16 lr_bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t lr_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t lr_u32x2 __attribute__((ext_vector_type(2)));

@@ -129,3 +129,73 @@ def test_infinities_in_the_gradients_of_a_bank(n, n_in, n_out, r, g, dtype):
             dt[i] = (up[k].float() * dy[i].float()).sum(1)
     check(ddown, dt, x)
     bank.close()
+
+
+def not_finite_banks(gen, inner, outer_, dtype):
+    """Three adapters of rank 2: one whose first inner row holds an infinity (and one more infinity in its second),
+    one of finite inner rows, one with infinities of both signs; every outer row cycles through infinities, NaN, zeros and
+    ordinary values, the second row shifted."""
+    a, b = zeros(3, 2, inner, dtype=dtype), zeros(3, 2, outer_, dtype=dtype)
+    a.uniform_(0.1, 1, generator=gen)
+    inf = float("inf")
+    a[0, 0, 1] = inf
+    a[2, 0, 0], a[2, 1, 1] = -inf, inf
+    cycle = torch.tensor([1.0, 0.0, inf, -inf, float("nan"), -2.0, 0.5], device=DEV).to(dtype)
+    at = torch.arange(outer_, device=DEV)
+    b[:, 0] = cycle[at % 7]
+    b[:, 1] = cycle[at // 7 % 7]
+    return a, b
+
+
+def adapted(src, w, inner, outer_, ids):
+    """src w^T + sum_r (inner_r src) outer_r in 64 bits, term by term."""
+    out = torch.empty(src.shape[0], w.shape[0], dtype=torch.float64, device=DEV)
+    size = torch.empty_like(out)
+    for i, k in enumerate(ids.tolist()):
+        s = src[i].double()
+        out[i], size[i] = w.double() @ s, w.double().abs() @ s.abs()
+        if k >= 0:
+            for r in range(2):
+                t = (inner[k, r].double() * s).sum()
+                out[i] += t * outer_[k, r].double()
+                size[i] += (t * outer_[k, r].double()).abs()
+    return out, size
+
+
+def same_kind(got, want, size, k):
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    inf = torch.isinf(want)
+    assert torch.equal(torch.isinf(got), inf) and torch.equal(got[inf].double(), want[inf])
+    fine = torch.isfinite(want)
+    unit = 2.0 ** -8 if got.dtype == BF else 0.0
+    bound = (4 * k ** 0.5 + 16) * 2.0 ** -24 * size + unit * want.abs()
+    assert bool(((got.double() - want).abs()[fine] <= bound[fine]).all())
+    assert bool(inf.any()) and bool(fine.any())
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("n,n_in,n_out", [(5, 24, 40), (50, 40, 31_000), (200, 24, 15_400), (150, 24, 61_500)])
+def test_infinities_on_both_sides_of_an_adapter(n, n_in, n_out, dtype):
+    """An adapter's low-rank value is infinite and its second matrix holds infinities, NaN and zeros: each result as
+    the formula says (an infinity times an infinity is one, times zero NaN), the other rows finite."""
+    from paper_2309_16743_amd import OT_BF16, OT_FP32, LowRankAdapters
+    print(f"infinities on both sides {n} {n_in} {n_out} {dtype}", flush=True)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(n)
+    bank = LowRankAdapters(n_in, n_out, 2, 3, precision=OT_BF16 if dtype == BF else OT_FP32, max_rows=n)
+    ids = (torch.arange(n, device=DEV) % 4 - 1).to(torch.int32)
+    w = zeros(n_out, n_in, dtype=dtype)
+    w.uniform_(-1, 1, generator=gen)
+    x, dy = zeros(n, n_in, dtype=dtype), zeros(n, n_out, dtype=dtype)
+    x.uniform_(0.1, 1, generator=gen)
+    down, up = not_finite_banks(gen, n_in, n_out, dtype)
+    y = zeros(n, n_out, dtype=dtype)
+    bank.forward(x, w, down, up, ids, y)
+    same_kind(y, *adapted(x, w, down, up, ids), n_in)
+    dy.uniform_(0.1, 1, generator=gen)
+    up, down = not_finite_banks(gen, n_out, n_in, dtype)
+    t, dx = torch.zeros(n, 2, device=DEV), zeros(n, n_in, dtype=dtype)
+    ddown, dup = zeros(3, 2, n_in, dtype=torch.float32), zeros(3, 2, n_out, dtype=torch.float32)
+    bank.backward(x, w, down, up, ids, dy, t, ddown, dup, dx=dx)
+    same_kind(dx, *adapted(dy, w.t(), up, down, ids), n_out)
+    bank.close()
