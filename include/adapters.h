@@ -38,7 +38,9 @@
  * Ownership: tensors are the caller's.  The object holds sizes and workspaces
  * (device memory on the device current at creation, which must be current in
  * every call).  Calls are asynchronous on the given stream; calls on one object
- * must not overlap, so a caller that changes streams orders them.  A call with
+ * must not overlap, so a caller that changes streams orders them.  The workspaces
+ * serve forwards and backwards alike: up to 272 bytes a row, and at most 0.5 GB of
+ * partial sums.  A call with
  * more than max_rows rows replaces the workspaces, which waits for the device
  * and is refused (OT_E_STATE) under stream capture; any other call allocates
  * nothing and may be captured.  Workspaces named by a captured call are kept

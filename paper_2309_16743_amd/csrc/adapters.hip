@@ -10,6 +10,7 @@
 #include <type_traits>
 #include <vector>
 
+#include "adapt_plan.h"
 #include "adapters.h"
 #include "common.h"
 #include "gemm_bf16.h"
@@ -118,6 +119,7 @@ struct ot_adapters {
   int32_t R, RP, G, precision;
   int device;
   int64_t max_rows;
+  ot::AdaptSizes sizes() const { return {in, out, RP, G, precision == OT_BF16}; }
   // workspaces of calls of up to max_rows rows, in one allocation
   unsigned char* ws = nullptr;
   bool captured = false;                    // a captured call may name ws
@@ -127,101 +129,6 @@ struct ot_adapters {
 namespace {
 
 constexpr int64_t kMaxRows = 1LL << 20;
-
-// Splits of the shrink's k range (length L) for n rows: enough blocks to fill the
-// card, each with at least 512 values (331 rows of 6561: 8.5 us, 15.6 with 2048); one when the range is short,
-// since the join costs a launch.  Blocks of unused slots (a large bank, few rows) are
-// not multiplied without bound.
-constexpr int64_t kShrinkBlocks = 1024;
-int64_t shrink_splits(int64_t n, int64_t L, int32_t G) {
-  if (L <= 4096) return 1;
-  const int64_t slots = ot::ceil_div(n, ot::kSlotRows) + std::min<int64_t>(G, n) / 2;
-  return std::max<int64_t>(1, std::min(std::min(ot::ceil_div(kShrinkBlocks, slots), L / 512),
-                                       32768 / (n / ot::kSlotRows + G + 1)));
-}
-
-// Block tiles (rows x columns): of gemm_bf16.h, then of gemm_f32x3.h.
-enum Tile : int {
-  kB64x64, kB64x128, kB128x128, kB256x256,
-  kX128x128, kX64x64, kX64x128, kX32x256, kX64x256
-};
-constexpr int kTileRows[] = {64, 64, 128, 256, 128, 64, 64, 32, 64};
-constexpr int kTileCols[] = {64, 128, 128, 256, 128, 64, 128, 256, 256};
-
-struct Plan {
-  int tile;
-  int64_t splits, k_chunk;
-};
-
-int64_t tiles_of(int tile, int64_t M, int64_t N) {
-  return ot::ceil_div(M, kTileRows[tile]) * ot::ceil_div(N, kTileCols[tile]);
-}
-
-// `want` splits of K, in k tiles of 64, as many as are not empty.
-Plan split_plan(int tile, int64_t K, int64_t want) {
-  Plan p{tile, 1, K};
-  if (want > 1) {
-    p.k_chunk = ot::ceil_div(ot::ceil_div(K, want), 64) * 64;
-    p.splits = ot::ceil_div(K, p.k_chunk);
-    if (p.splits == 1) p.k_chunk = K;
-  }
-  return p;
-}
-
-// Tile and splits by the number of blocks that each choice gives (us of the whole call, as measured with each
-// tile for all products of the kind):
-// bf16 layers: 1024 x 1000000 x 2048 on 64 x 64, 64 x 128, 128 x 128, 256 x 256 tiles 8529, 7111, 6277, 4700: the
-//   largest tile that still gives about a block per CU.  16 x 1000000 x 1024 on the same 678, 538, 638, 755: few
-//   rows stream the weights and want the blocks' loads, not their products.  1024 x 2048 x 2048 37.5, 38.9,
-//   51.9, 82.7: small tiles until every CU has blocks.
-// bf16 input gradients: 512 x 1024, k 1000000 on 256 x 256 tiles in 16, 32, 64 splits 2207, 1677, 1708, on
-//   128 x 128 2216, 2104, 2214: about a block per CU.  1024 x 2048, k 2048 on 64 x 128 tiles whole 51, in
-//   2 splits 55 (the join is a launch).
-// fp32 layers: 1024 x 10000 x 256 on 64 x 64, 64 x 128, 128 x 128 tiles 71, 66, 74.
-// fp32 input gradients (the product alone): 331 x 437, k 6561 on 128 x 128 tiles in 12, 28, 42, 60 splits 64, 41,
-//   35, 38; on 64 x 64 in 28, 60 41, 37.
-// A plan depends on the rows only through whole groups of 32 (part_values).
-Plan plan_expand(bool bf16, bool kmajor, int64_t M, int64_t N, int64_t K) {
-  constexpr int64_t kCUs = 256;
-  if (bf16) {
-    if (kmajor) {
-      if (M > 128 && tiles_of(kB256x256, M, N) >= kCUs - 16) return split_plan(kB256x256, K, 1);
-      if (M <= 64 && tiles_of(kB64x128, M, N) >= kCUs - 16) return split_plan(kB64x128, K, 1);
-      if (tiles_of(kB128x128, M, N) >= 2 * kCUs - 32) return split_plan(kB128x128, K, 1);
-      if (tiles_of(kB64x128, M, N) >= 2 * kCUs - 32) return split_plan(kB64x128, K, 1);
-      return split_plan(kB64x64, K, 1);
-    }
-    const int big = M > 128 ? kB256x256 : M > 64 ? kB128x128 : kB64x128;
-    const int64_t t = tiles_of(big, M, N), sp = ot::ceil_div(kCUs - 16, t);
-    if (K / sp >= 2048) return split_plan(big, K, sp);
-    const int64_t t2 = tiles_of(kB64x128, M, N);
-    return split_plan(kB64x128, K, std::max<int64_t>(1, std::min(ot::ceil_div(kCUs - 16, t2), K / 512)));
-  }
-  if (kmajor) {
-    if (M <= 32 && tiles_of(kX32x256, M, N) >= kCUs) return split_plan(kX32x256, K, 1);
-    if (M <= 64 && tiles_of(kX64x256, M, N) >= kCUs) return split_plan(kX64x256, K, 1);
-    return split_plan(tiles_of(kX64x128, M, N) >= 2 * kCUs ? kX64x128 : kX64x64, K, 1);
-  }
-  const int tile = M <= 32 && N > 128 ? kX32x256 : M <= 64 && N > 128 ? kX64x256 : M <= 64 || N <= 64 ? kX64x64 : kX128x128;
-  return split_plan(tile, K, std::max<int64_t>(1, std::min(2 * kCUs / tiles_of(tile, M, N), K / 128)));
-}
-
-// Partial sums of the plan (fp32 values; 0: not split).
-int64_t plan_values(const Plan& p, int64_t M, int64_t N) { return p.splits > 1 ? p.splits * M * ((N + 3) / 4 * 4) : 0; }
-
-// The one launch over a long dy keeps a partial of every row and column range, so that its
-// workspace grows with rows times columns: it takes batches of up to this many rows.
-constexpr int64_t kPassMaxRows = 4096;
-
-// Pieces of 64 columns per wavefront in that launch (0: dy is short and takes the two
-// products apart).  512 rows, 8 adapters of rank 16, all launches but the input gradient, in it and
-// apart: 8192 columns 27.2 and 26.4 us, 16384 31.0 and 32.7 (fp32 41.2 and 40.7), 65536 56 and 67
-// (fp32 98 and 110; rank 64 147 and 322), 131072 88 and 123.
-int pass_chunks(int64_t L, int32_t G) {
-  if (L < 16384) return 0;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(4, L / 512 * G / 1024));
-}
-int64_t pass_ranges(int64_t L, int32_t G) { return ot::ceil_div(L, (int64_t)pass_chunks(L, G) * ot::kPassThreads); }
 
 struct Work {
   int32_t* perm;
@@ -242,17 +149,6 @@ int slot_rows(int64_t L) { return L <= 4096 ? kMinSlotRows : ot::kSlotRows; }
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// Partial sums that a call of up to n rows needs.
-int64_t part_values(const ot_adapters* a, int64_t n) {
-  // shrinks: splits * rows, with splits <= kShrinkBlocks / (rows / 32) + 1
-  int64_t most = std::max(a->in, a->out) > 4096 ? (kShrinkBlocks * ot::kSlotRows + n) * a->RP : 0;
-  if (pass_chunks(a->out, a->G)) most = std::max(most, pass_ranges(a->out, a->G) * std::min(n, kPassMaxRows) * a->RP);
-  // the input gradient: a plan depends on the rows only through whole groups of 32
-  for (int64_t m = 32; m < n + 32; m += 32)
-    most = std::max(most, plan_values(plan_expand(a->precision == OT_BF16, false, m, a->in, a->out), m, a->in));
-  return most;
-}
-
 // Workspace of a call of n rows at `base`; returns its size.
 int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
   int64_t at = 0;
@@ -268,7 +164,7 @@ int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
   t.off = reinterpret_cast<int32_t*>(take(4 * (a->G + 2)));
   t.slots = reinterpret_cast<ot::RowSlot*>(take((int64_t)sizeof(ot::RowSlot) * t.n_slots));
   t.ts = reinterpret_cast<float*>(take(4 * n * a->RP));
-  t.part = reinterpret_cast<float*>(take(4 * part_values(a, n)));
+  t.part = reinterpret_cast<float*>(take(4 * ot::part_values(a->sizes(), n)));
   if (w) *w = t;
   return at;
 }
@@ -345,7 +241,7 @@ int run_shrink(const ot_adapters* a, ot::ShrinkArgs s, const int32_t* ids, int64
   const bool self = self_sorted(n, s.G);
   int rc;
   if (!self && (rc = run_group(a, ids, n, s.L, w, st))) return rc;
-  const int64_t splits = shrink_splits(n, s.L, s.G);
+  const int64_t splits = ot::shrink_splits(n, s.L, s.G);
   s.k_chunk = ot::ceil_div(ot::ceil_div(s.L, splits), ot::kShrinkUnit) * ot::kShrinkUnit;
   s.splits = (int32_t)ot::ceil_div(s.L, s.k_chunk);
   s.n = n;
@@ -375,8 +271,8 @@ int run_shrink(const ot_adapters* a, ot::ShrinkArgs s, const int32_t* ids, int64
 template <class T>
 int run_pass(const ot_adapters* a, const ot::OuterArgs& o, const void* up, int64_t ldu, int64_t n, const Work& w,
              hipStream_t st) {
-  const int chunks = pass_chunks(a->out, a->G);
-  const int64_t ranges = pass_ranges(a->out, a->G);
+  const int chunks = ot::pass_chunks(a->sizes(), n);
+  const int64_t ranges = ot::pass_ranges(a->sizes(), n);
   const ot::PassArgs p{o, up, ldu, w.part, n, ranges, a->RP, chunks};
   const dim3 grid((unsigned)(ot::ceil_div(ranges, 8) * 16), (unsigned)a->G), block(ot::kPassThreads);
   switch (a->RP / 16) {
@@ -431,25 +327,25 @@ template <ot::LayB LB, ot::EpiB E>
 hipError_t launch_b(int tile, const ot::GemmBArgs& g, int64_t splits, hipStream_t st) {
   constexpr ot::LayB KM = ot::LayB::KMajor;
   if constexpr (LB == KM) {
-    if (tile == kB64x64) return ot::launch_gemm_bf16_pipe<64, 64, 64, 4, 2, KM, LB, E>(g, splits, st);
+    if (tile == ot::kB64x64) return ot::launch_gemm_bf16_pipe<64, 64, 64, 4, 2, KM, LB, E>(g, splits, st);
   }
-  if (tile == kB64x128) return ot::launch_gemm_bf16_pipe<64, 128, 64, 3, 4, KM, LB, E, 4>(g, splits, st);
-  if (tile == kB128x128) return ot::launch_gemm_bf16_pipe<128, 128, 32, 4, 2, KM, LB, E>(g, splits, st);
+  if (tile == ot::kB64x128) return ot::launch_gemm_bf16_pipe<64, 128, 64, 3, 4, KM, LB, E, 4>(g, splits, st);
+  if (tile == ot::kB128x128) return ot::launch_gemm_bf16_pipe<128, 128, 32, 4, 2, KM, LB, E>(g, splits, st);
   return ot::launch_gemm_bf16_pp<4, KM, LB, E>(g, splits, st);
 }
 
 template <ot::Lay LB, ot::Epi E>
 hipError_t launch_x(int tile, const ot::GemmArgs& g, int64_t splits, hipStream_t st) {
   constexpr ot::Lay KM = ot::Lay::KMajor;
-  if (tile == kX64x64) return ot::launch_gemm_f32x3<2, 2, 1, 1, KM, LB, E>(g, splits, st);
-  if (tile == kX64x128) return ot::launch_gemm_f32x3<2, 2, 1, 2, KM, LB, E>(g, splits, st);
-  if (tile == kX32x256) return ot::launch_gemm_f32x3<1, 4, 1, 2, KM, LB, E>(g, splits, st);
-  if (tile == kX64x256) return ot::launch_gemm_f32x3<1, 4, 2, 2, KM, LB, E>(g, splits, st);
+  if (tile == ot::kX64x64) return ot::launch_gemm_f32x3<2, 2, 1, 1, KM, LB, E>(g, splits, st);
+  if (tile == ot::kX64x128) return ot::launch_gemm_f32x3<2, 2, 1, 2, KM, LB, E>(g, splits, st);
+  if (tile == ot::kX32x256) return ot::launch_gemm_f32x3<1, 4, 1, 2, KM, LB, E>(g, splits, st);
+  if (tile == ot::kX64x256) return ot::launch_gemm_f32x3<1, 4, 2, 2, KM, LB, E>(g, splits, st);
   return ot::launch_gemm_f32x3<2, 2, 2, 2, KM, LB, E>(g, splits, st);
 }
 
 template <class T, class G>
-int reduce_splits(const Expand& e, const G& g, const Plan& p, const float* part, hipStream_t st) {
+int reduce_splits(const Expand& e, const G& g, const ot::AdaptPlan& p, const float* part, hipStream_t st) {
   hipLaunchKernelGGL(ot::adapt_reduce_kernel<T>, dim3((unsigned)ot::ceil_div(e.M * ((e.N + 3) / 4), 256)), dim3(256), 0,
                      st, part, (int32_t)p.splits, g.split_stride, e.M, e.N, g.ldc, e.lr.perm,
                      static_cast<const T*>(e.lr.mask), e.lr.ldmask, static_cast<T*>(e.C), e.ldc);
@@ -459,7 +355,7 @@ int reduce_splits(const Expand& e, const G& g, const Plan& p, const float* part,
 
 // part: workspace of plan_values() floats.  Split products only as input gradients.
 template <class G>
-void fill_expand(G& g, const Expand& e, const Plan& p, float* part) {
+void fill_expand(G& g, const Expand& e, const ot::AdaptPlan& p, float* part) {
   g.lda = e.lda;
   g.ldb = e.ldb;
   g.ldc = e.ldc;
@@ -476,7 +372,7 @@ void fill_expand(G& g, const Expand& e, const Plan& p, float* part) {
 }
 
 int run_expand(const Expand& e, bool bf16, bool kmajor, float* part, hipStream_t st) {
-  const Plan p = plan_expand(bf16, kmajor, e.M, e.N, e.K);
+  const ot::AdaptPlan p = ot::plan_expand(bf16, kmajor, e.M, e.N, e.K);
   hipError_t rc;
   if (bf16) {
     ot::GemmBArgs g{};
@@ -626,7 +522,7 @@ extern "C" int adapters_backward(ot_adapters* a, const void* x, int64_t ldx, con
     if ((rc = run_group(a, ids, n, a->out, wk, st))) return rc;
     return e == 2 ? run_outer<uint16_t>(ou, od, n, a->G, st) : run_outer<float>(ou, od, n, a->G, st);
   }
-  const bool pass = n <= kPassMaxRows && pass_chunks(a->out, a->G) > 0;
+  const bool pass = ot::pass_chunks(a->sizes(), n) > 0;
   if (pass) {
     if ((rc = run_group(a, ids, n, a->out, wk, st))) return rc;
     rc = e == 2 ? run_pass<uint16_t>(a, ou, up, ldu, n, wk, st) : run_pass<float>(a, ou, up, ldu, n, wk, st);

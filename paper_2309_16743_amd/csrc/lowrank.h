@@ -17,13 +17,12 @@
 
 #include <type_traits>
 
+#include "adapt_plan.h"
 #include "common.h"
 #include "intmath.h"
 #include "lowrank_ops.h"
 
 namespace ot {
-
-constexpr int kSlotRows = 32;       // sorted rows of one adapter that a block takes together, at most
 
 // Rows [start, start + count) of the sorted order, all of adapter g.
 struct RowSlot {
@@ -480,7 +479,7 @@ __device__ __forceinline__ void outer_block(const OuterArgs& a, int64_t block, i
 // dt: a wavefront takes 32 rows and its part of the columns, the block joins in LDS, and
 //   one partial per block goes to memory.
 // grid = (16 per 8 column ranges, adapters), 512 threads.
-constexpr int kPassRows = 128, kPassThreads = 512;
+constexpr int kPassRows = 128;
 struct PassArgs {
   OuterArgs o;            // src = dy, coef = t by row, out = dup
   const void* up;         // G x R rows of L values
