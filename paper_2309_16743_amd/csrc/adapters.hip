@@ -149,7 +149,8 @@ int slot_rows(int64_t L) { return L <= 4096 ? kMinSlotRows : ot::kSlotRows; }
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// Workspace of a call of n rows at `base`; returns its size.
+// Workspace of a call of n rows at `base`; returns the size of what comes before the partial sums, whose
+// size only allocate() needs (part_values looks at every group of 32 rows: 0.1 ms and more at 2^20).
 int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -164,14 +165,14 @@ int64_t layout(const ot_adapters* a, int64_t n, unsigned char* base, Work* w) {
   t.off = reinterpret_cast<int32_t*>(take(4 * (a->G + 2)));
   t.slots = reinterpret_cast<ot::RowSlot*>(take((int64_t)sizeof(ot::RowSlot) * t.n_slots));
   t.ts = reinterpret_cast<float*>(take(4 * n * a->RP));
-  t.part = reinterpret_cast<float*>(take(4 * ot::part_values(a->sizes(), n)));
+  t.part = reinterpret_cast<float*>(base + at);
   if (w) *w = t;
   return at;
 }
 
 int allocate(ot_adapters* a, int64_t rows, const char* what) {
   unsigned char* p = nullptr;
-  const int64_t bytes = layout(a, rows, nullptr, nullptr);
+  const int64_t bytes = layout(a, rows, nullptr, nullptr) + 4 * ot::part_values(a->sizes(), rows);
   const hipError_t e = hipMalloc(reinterpret_cast<void**>(&p), (size_t)bytes);
   if (e != hipSuccess) {
     (void)hipGetLastError();

@@ -59,3 +59,31 @@ def test_many_rows_of_a_long_gradient(n, n_out, rank, g, dtype):
         bound = (4 * (n_out + n) ** 0.5 + 16) * 2.0 ** -24 * (dt_size.t() @ xk.abs())
         assert bool(((ddown[k].double() - dt.t() @ xk).abs() <= bound).all())
     bank.close()
+
+
+def test_host_time_of_a_call_does_not_grow_with_its_rows():
+    """A call needs the address of its partial sums, not their size (which looks at the plan of every group of 32
+    rows): the host's time for 2^20 rows is that for 32 rows within 40 us (the shortest of 20 calls each)."""
+    import time
+
+    from paper_2309_16743_amd import LowRankAdapters
+    n = 1 << 20
+    x, w, y = (torch.zeros(r, 8, device=DEV) for r in (n, 8, n))
+    down, up = torch.zeros(1, 1, 8, device=DEV), torch.zeros(1, 1, 8, device=DEV)
+    ids = torch.zeros(n, dtype=torch.int32, device=DEV)
+    bank = LowRankAdapters(8, 8, 1, 1, max_rows=n)
+
+    def shortest(rows):
+        best = 1.0
+        for _ in range(20):
+            torch.cuda.synchronize()
+            t0 = time.perf_counter()
+            bank.forward(x[:rows], w, down, up, ids[:rows], y[:rows])
+            best = min(best, time.perf_counter() - t0)
+        return best
+
+    few, many = shortest(32), shortest(n)
+    torch.cuda.synchronize()
+    print(f"host time of a call of 32 rows {few * 1e6:.0f} us, of 2^20 {many * 1e6:.0f} us", flush=True)
+    bank.close()
+    assert many < few + 40e-6
