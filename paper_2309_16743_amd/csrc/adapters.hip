@@ -324,6 +324,7 @@ struct Expand {
   ot::AdaptRows lr;
 };
 
+// The tiles that plan_expand gives for each layout.
 template <ot::LayB LB, ot::EpiB E>
 hipError_t launch_b(int tile, const ot::GemmBArgs& g, int64_t splits, hipStream_t st) {
   constexpr ot::LayB KM = ot::LayB::KMajor;
@@ -332,17 +333,22 @@ hipError_t launch_b(int tile, const ot::GemmBArgs& g, int64_t splits, hipStream_
   }
   if (tile == ot::kB64x128) return ot::launch_gemm_bf16_pipe<64, 128, 64, 3, 4, KM, LB, E, 4>(g, splits, st);
   if (tile == ot::kB128x128) return ot::launch_gemm_bf16_pipe<128, 128, 32, 4, 2, KM, LB, E>(g, splits, st);
-  return ot::launch_gemm_bf16_pp<4, KM, LB, E>(g, splits, st);
+  if (tile == ot::kB256x256) return ot::launch_gemm_bf16_pp<4, KM, LB, E>(g, splits, st);
+  return hipErrorInvalidValue;
 }
 
 template <ot::Lay LB, ot::Epi E>
 hipError_t launch_x(int tile, const ot::GemmArgs& g, int64_t splits, hipStream_t st) {
   constexpr ot::Lay KM = ot::Lay::KMajor;
   if (tile == ot::kX64x64) return ot::launch_gemm_f32x3<2, 2, 1, 1, KM, LB, E>(g, splits, st);
-  if (tile == ot::kX64x128) return ot::launch_gemm_f32x3<2, 2, 1, 2, KM, LB, E>(g, splits, st);
   if (tile == ot::kX32x256) return ot::launch_gemm_f32x3<1, 4, 1, 2, KM, LB, E>(g, splits, st);
   if (tile == ot::kX64x256) return ot::launch_gemm_f32x3<1, 4, 2, 2, KM, LB, E>(g, splits, st);
-  return ot::launch_gemm_f32x3<2, 2, 2, 2, KM, LB, E>(g, splits, st);
+  if constexpr (LB == KM) {
+    if (tile == ot::kX64x128) return ot::launch_gemm_f32x3<2, 2, 1, 2, KM, LB, E>(g, splits, st);
+  } else {
+    if (tile == ot::kX128x128) return ot::launch_gemm_f32x3<2, 2, 2, 2, KM, LB, E>(g, splits, st);
+  }
+  return hipErrorInvalidValue;
 }
 
 template <class T, class G>

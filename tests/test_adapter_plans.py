@@ -41,3 +41,16 @@ def test_workspace_covers_every_call_and_is_bounded(tmp_path):
 def test_rows_alone_do_not_bound_the_pass(tmp_path):
     res = run(build(tmp_path, "-DROWS_ONLY"), "bound")
     assert res.returncode == 1 and "values for" in res.stdout, res.stdout[-2000:]
+
+
+def test_the_gpu_tests_run_every_kernel(tmp_path):
+    """Each product kernel and each way of the low-rank products that some call takes is taken by one of the tested
+    sizes (test_gpu_adapters_tiles)."""
+    from adapter_sizes import SIZES
+    exe = build(tmp_path)
+    every = set(run(exe, "kernels").stdout.splitlines())
+    assert len(every) > 20
+    seen = set()
+    for size in SIZES:
+        seen |= set(run(exe, "of", *map(str, size)).stdout.splitlines())
+    assert seen == every, sorted(every ^ seen)
