@@ -313,19 +313,19 @@ class Surrogate:
 
 
 # A small call's time is the host's, so the checks below ask each tensor for each of its properties once.
-def _matrix(t, rows: int, cols: int, dtype, what: str):
-    """(pointer, leading dimension) of a rows x cols device tensor with unit column stride."""
+def _matrix(t, rows: int, cols: int, dtype, device: int, what: str):
+    """(pointer, leading dimension) of a rows x cols tensor on the device with unit column stride."""
     shape, st = t.shape, t.stride()
     if t.dtype is not dtype or len(shape) != 2 or shape[0] != rows or shape[1] != cols or (
             rows > 0 and cols > 1 and st[1] != 1):
         raise ValueError(f"{what}: expected a {rows} x {cols} {dtype} tensor with unit column stride")
-    if not t.is_cuda:
-        raise ValueError(f"{what}: expected a device tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: expected a tensor on cuda:{device}")
     return t.data_ptr(), st[0] if rows > 1 else max(st[0], cols)
 
 
-def _bank(t, n: int, rank: int, cols: int, dtype, what: str):
-    """(pointer, leading dimension) of an n x rank x cols device tensor whose rows follow each other."""
+def _bank(t, n: int, rank: int, cols: int, dtype, device: int, what: str):
+    """(pointer, leading dimension) of an n x rank x cols tensor on the device whose rows follow each other."""
     shape, st = t.shape, t.stride()
     if t.dtype is not dtype or len(shape) != 3 or shape[0] != n or shape[1] != rank or shape[2] != cols or (
             cols > 1 and st[2] != 1):
@@ -333,19 +333,19 @@ def _bank(t, n: int, rank: int, cols: int, dtype, what: str):
     ld = st[1] if rank > 1 else st[0] if n > 1 else max(st[0], cols)
     if n > 1 and st[0] != rank * ld:
         raise ValueError(f"{what}: the rows of successive adapters must follow each other")
-    if not t.is_cuda:
-        raise ValueError(f"{what}: expected a device tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: expected a tensor on cuda:{device}")
     return t.data_ptr(), ld
 
 
-def _vector(t, n: int, dtype, what: str):
+def _vector(t, n: int, dtype, device: int, what: str):
     if t is None:
         return None
     shape = t.shape
     if t.dtype is not dtype or len(shape) != 1 or shape[0] != n or (n > 1 and t.stride()[0] != 1):
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {n} values")
-    if not t.is_cuda:
-        raise ValueError(f"{what}: expected a device tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: expected a tensor on cuda:{device}")
     return t.data_ptr()
 
 
@@ -368,7 +368,7 @@ class LowRankAdapters:
         check("adapters_create", load().adapters_create(C.byref(h), in_dim, out_dim, rank, n_adapters, precision,
                                                         max_rows))
         self._h = h
-        self._torch, self._lib = torch, load()
+        self._torch, self._lib, self._device = torch, load(), torch.cuda.current_device()
         self.in_dim, self.out_dim, self.rank, self.n_adapters = in_dim, out_dim, rank, n_adapters
         self.precision = precision
         self.dtype = torch.bfloat16 if precision == OT_BF16 else torch.float32
@@ -378,27 +378,27 @@ class LowRankAdapters:
         return self._h
 
     def _common(self, x, down, up, ids, scale):
-        torch = self._torch
+        torch, dev = self._torch, self._device
         n = x.shape[0]
         g, r = self.n_adapters, self.rank
-        return (n, _matrix(x, n, self.in_dim, self.dtype, "x"),
-                (None, 0) if down is None else _bank(down, g, r, self.in_dim, self.dtype, "down"),
-                _bank(up, g, r, self.out_dim, self.dtype, "up"),
-                _vector(ids, n, torch.int32, "ids"), _vector(scale, g, torch.float32, "scale"))
+        return (n, _matrix(x, n, self.in_dim, self.dtype, dev, "x"),
+                (None, 0) if down is None else _bank(down, g, r, self.in_dim, self.dtype, dev, "down"),
+                _bank(up, g, r, self.out_dim, self.dtype, dev, "up"),
+                _vector(ids, n, torch.int32, dev, "ids"), _vector(scale, g, torch.float32, dev, "scale"))
 
     def forward(self, x, w, down, up, ids, y, bias=None, scale=None, t=None, relu: bool = False, stream=None) -> None:
         """y = x W^T + bias + scale (x down^T) up per row's adapter (ids), in y's type
         (float32 or bfloat16); t receives x down^T for backward()."""
-        torch = self._torch
+        torch, dev = self._torch, self._device
         n, xp, dp, up_, ip, sp = self._common(x, down, up, ids, scale)
-        wp = _matrix(w, self.out_dim, self.in_dim, self.dtype, "w")
+        wp = _matrix(w, self.out_dim, self.in_dim, self.dtype, dev, "w")
         y_type = y.dtype
         if y_type is not torch.float32 and y_type is not torch.bfloat16:
             raise ValueError("y: expected float32 or bfloat16")
-        yp = _matrix(y, n, self.out_dim, y_type, "y")
-        tp = (None, 0) if t is None else _matrix(t, n, self.rank, torch.float32, "t")
+        yp = _matrix(y, n, self.out_dim, y_type, dev, "y")
+        tp = (None, 0) if t is None else _matrix(t, n, self.rank, torch.float32, dev, "t")
         check("adapters_forward", self._lib.adapters_forward(
-            self._h, *xp, *wp, _vector(bias, self.out_dim, torch.float32, "bias"), *dp, *up_, sp, ip, n, *yp,
+            self._h, *xp, *wp, _vector(bias, self.out_dim, torch.float32, dev, "bias"), *dp, *up_, sp, ip, n, *yp,
             OT_BF16 if y_type is torch.bfloat16 else OT_FP32, *tp, OT_ADAPTERS_RELU if relu else 0,
             _raw_stream(stream, self._torch)))
 
@@ -406,17 +406,17 @@ class LowRankAdapters:
                  stream=None) -> None:
         """Gradients of the bank into ddown, dup (fp32, whole) and, if given, of x into dx
         (relu_input: zero where x is not above 0); w and down may be None without dx."""
-        torch = self._torch
+        torch, dev = self._torch, self._device
         n, xp, dp, up_, ip, sp = self._common(x, down, up, ids, scale)
         g, r = self.n_adapters, self.rank
         if dx is not None and (w is None or down is None):
             raise ValueError("dx needs w and down")
-        wp = (None, 0) if w is None else _matrix(w, self.out_dim, self.in_dim, self.dtype, "w")
-        dyp = _matrix(dy, n, self.out_dim, self.dtype, "dy")
-        tp = _matrix(t, n, r, torch.float32, "t")
-        ddp = _bank(ddown, g, r, self.in_dim, torch.float32, "ddown")
-        dup_ = _bank(dup, g, r, self.out_dim, torch.float32, "dup")
-        dxp = (None, 0) if dx is None else _matrix(dx, n, self.in_dim, self.dtype, "dx")
+        wp = (None, 0) if w is None else _matrix(w, self.out_dim, self.in_dim, self.dtype, dev, "w")
+        dyp = _matrix(dy, n, self.out_dim, self.dtype, dev, "dy")
+        tp = _matrix(t, n, r, torch.float32, dev, "t")
+        ddp = _bank(ddown, g, r, self.in_dim, torch.float32, dev, "ddown")
+        dup_ = _bank(dup, g, r, self.out_dim, torch.float32, dev, "dup")
+        dxp = (None, 0) if dx is None else _matrix(dx, n, self.in_dim, self.dtype, dev, "dx")
         check("adapters_backward", self._lib.adapters_backward(
             self._h, *xp, *wp, *dp, *up_, sp, ip, n, *dyp, *tp, *ddp, *dup_, *dxp,
             OT_ADAPTERS_RELU_INPUT if relu_input else 0, _raw_stream(stream, self._torch)))
@@ -433,7 +433,7 @@ class LowRankAdapters:
             pass
 
 
-def _list_arrays(tensors, dtypes, counts, what: str):
+def _list_arrays(tensors, dtypes, counts, device: int, what: str):
     """Host array of the device addresses of a list of contiguous tensors (None: NULL entries allowed)."""
     if len(tensors) != len(counts):
         raise ValueError(f"{what}: expected {len(counts)} tensors")
@@ -443,7 +443,9 @@ def _list_arrays(tensors, dtypes, counts, what: str):
             continue
         if t.dtype != dtypes[i] or t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{what}[{i}]: expected a contiguous {dtypes[i]} tensor of {n} elements")
-        out[i] = _dev_ptr(t) if n else None
+        if n and t.get_device() != device:
+            raise ValueError(f"{what}[{i}]: expected a tensor on cuda:{device}")
+        out[i] = t.data_ptr() if n else None
     return out
 
 
@@ -464,8 +466,9 @@ class GradientClip:
                 raise ValueError(f"grads[{i}]: expected float32 or bfloat16")
             types[i] = OT_BF16 if t.dtype == torch.bfloat16 else OT_FP32
         dtypes = [t.dtype for t in self.grads]
-        g = _list_arrays(self.grads, dtypes, counts, "grads")
-        o = None if self.out is None else _list_arrays(self.out, dtypes, counts, "out")
+        self._device = torch.cuda.current_device()
+        g = _list_arrays(self.grads, dtypes, counts, self._device, "grads")
+        o = None if self.out is None else _list_arrays(self.out, dtypes, counts, self._device, "out")
         h = C.c_void_p()
         check("clip_create", load().clip_create(C.byref(h), n, g, o, counts, types))
         self._h = h
@@ -473,11 +476,13 @@ class GradientClip:
 
     def norm(self, norm, stream=None) -> None:
         """The global norm into the device scalar `norm`."""
-        check("clip_norm", self._lib.clip_norm(self._h, _scalar(norm, "norm", self._torch), _raw_stream(stream, self._torch)))
+        check("clip_norm", self._lib.clip_norm(self._h, _scalar(norm, "norm", self._device, self._torch),
+                                               _raw_stream(stream, self._torch)))
 
     def apply(self, max_norm: float, norm=None, stream=None) -> None:
         """Scale every tensor by min(1, max_norm / norm); the norm into `norm` (nullable)."""
-        check("clip_apply", self._lib.clip_apply(self._h, max_norm, _scalar(norm, "norm", self._torch), _raw_stream(stream, self._torch)))
+        check("clip_apply", self._lib.clip_apply(self._h, max_norm, _scalar(norm, "norm", self._device, self._torch),
+                                                 _raw_stream(stream, self._torch)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -491,12 +496,14 @@ class GradientClip:
             pass
 
 
-def _scalar(t, what: str, torch):
+def _scalar(t, what: str, device: int, torch):
     if t is None:
         return None
     if t.dtype is not torch.float32 or t.numel() != 1:
         raise ValueError(f"{what}: expected a float32 tensor of one element")
-    return _dev_ptr(t)
+    if t.get_device() != device:
+        raise ValueError(f"{what}: expected a tensor on cuda:{device}")
+    return t.data_ptr()
 
 
 class AdamTensors:
@@ -510,6 +517,7 @@ class AdamTensors:
         self.params, self.grads, self.m, self.v = list(params), list(grads), list(m), list(v)
         self.copies = None if copies is None else list(copies)
         n = len(self.params)
+        self._device = torch.cuda.current_device()
         counts = (C.c_int64 * n)(*[t.numel() for t in self.params])
         f32 = [torch.float32] * n
         arrays = []
@@ -517,8 +525,10 @@ class AdamTensors:
             tensors = getattr(self, name)
             if any(t is None for t in tensors):
                 raise ValueError(f"{name}: None among the tensors")
-            arrays.append(_list_arrays(tensors, f32, counts, name))
-        c = None if self.copies is None else _list_arrays(self.copies, [torch.bfloat16] * n, counts, "copies")
+            arrays.append(_list_arrays(tensors, f32, counts, self._device, name))
+        c = None
+        if self.copies is not None:
+            c = _list_arrays(self.copies, [torch.bfloat16] * n, counts, self._device, "copies")
         h = C.c_void_p()
         check("adam_create", load().adam_create(C.byref(h), n, *arrays, c, counts, lr, beta1, beta2, eps, steps))
         self._h = h
@@ -527,7 +537,8 @@ class AdamTensors:
     def step(self, max_norm: float = 0.0, norm=None, stream=None) -> None:
         """One step; max_norm 0: gradients as they are.  norm (nullable): the norm before
         clipping.  A norm that is not finite takes no step."""
-        check("adam_step", self._lib.adam_step(self._h, max_norm, _scalar(norm, "norm", self._torch), _raw_stream(stream, self._torch)))
+        check("adam_step", self._lib.adam_step(self._h, max_norm, _scalar(norm, "norm", self._device, self._torch),
+                                               _raw_stream(stream, self._torch)))
 
     def set_lr(self, lr: float) -> None:
         check("adam_set_lr", load().adam_set_lr(self._h, lr))
