@@ -349,10 +349,12 @@ def _vector(t, n: int, dtype, device: int, what: str):
     return t.data_ptr()
 
 
-def _raw_stream(stream, torch):
-    """Handle of the given stream, or of the current one (without making a Stream object for it)."""
+def _raw_stream(stream, device: int, torch):
+    """Handle of the given stream, or of the device's current one: without making a Stream object for it (1 us of a
+    small call) where torch can say it."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        current = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream(device).cuda_stream if current is None else current(device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -400,7 +402,7 @@ class LowRankAdapters:
         check("adapters_forward", self._lib.adapters_forward(
             self._h, *xp, *wp, _vector(bias, self.out_dim, torch.float32, dev, "bias"), *dp, *up_, sp, ip, n, *yp,
             OT_BF16 if y_type is torch.bfloat16 else OT_FP32, *tp, OT_ADAPTERS_RELU if relu else 0,
-            _raw_stream(stream, self._torch)))
+            _raw_stream(stream, self._device, self._torch)))
 
     def backward(self, x, w, down, up, ids, dy, t, ddown, dup, dx=None, scale=None, relu_input: bool = False,
                  stream=None) -> None:
@@ -419,7 +421,7 @@ class LowRankAdapters:
         dxp = (None, 0) if dx is None else _matrix(dx, n, self.in_dim, self.dtype, dev, "dx")
         check("adapters_backward", self._lib.adapters_backward(
             self._h, *xp, *wp, *dp, *up_, sp, ip, n, *dyp, *tp, *ddp, *dup_, *dxp,
-            OT_ADAPTERS_RELU_INPUT if relu_input else 0, _raw_stream(stream, self._torch)))
+            OT_ADAPTERS_RELU_INPUT if relu_input else 0, _raw_stream(stream, self._device, self._torch)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -477,12 +479,12 @@ class GradientClip:
     def norm(self, norm, stream=None) -> None:
         """The global norm into the device scalar `norm`."""
         check("clip_norm", self._lib.clip_norm(self._h, _scalar(norm, "norm", self._device, self._torch),
-                                               _raw_stream(stream, self._torch)))
+                                               _raw_stream(stream, self._device, self._torch)))
 
     def apply(self, max_norm: float, norm=None, stream=None) -> None:
         """Scale every tensor by min(1, max_norm / norm); the norm into `norm` (nullable)."""
         check("clip_apply", self._lib.clip_apply(self._h, max_norm, _scalar(norm, "norm", self._device, self._torch),
-                                                 _raw_stream(stream, self._torch)))
+                                                 _raw_stream(stream, self._device, self._torch)))
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:
@@ -538,7 +540,7 @@ class AdamTensors:
         """One step; max_norm 0: gradients as they are.  norm (nullable): the norm before
         clipping.  A norm that is not finite takes no step."""
         check("adam_step", self._lib.adam_step(self._h, max_norm, _scalar(norm, "norm", self._device, self._torch),
-                                               _raw_stream(stream, self._torch)))
+                                               _raw_stream(stream, self._device, self._torch)))
 
     def set_lr(self, lr: float) -> None:
         check("adam_set_lr", load().adam_set_lr(self._h, lr))
