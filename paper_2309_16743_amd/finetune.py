@@ -150,9 +150,13 @@ class AdapterTrainer:
             self._forward(x, ids, out=y)
 
     def train_step(self, x, u, ids) -> None:
-        """One step on rows x -> u of ensembles ids: mean squared error, gradients of every adapter, clipping,
-        Adam.  self.loss and self.norm receive the loss and the gradients' norm before clipping."""
+        """One step on 1 to `batch` rows x -> u of ensembles ids: mean squared error, gradients of every adapter,
+        clipping, Adam.  self.loss and self.norm receive the loss and the gradients' norm before clipping."""
         n = x.shape[0]
+        if n < 1:
+            raise ValueError("x: expected at least one row")
+        if tuple(u.shape) != (n, self.widths[-1]):
+            raise ValueError(f"u: expected a {n} x {self.widths[-1]} tensor")
         with self._ordered():
             y = self._forward(x, ids, save=True)
             r = y - u
