@@ -64,7 +64,7 @@ class AdapterTrainer:
             gen = torch.Generator(device=dev)
             gen.manual_seed(seed)
             self.scale = torch.full((n_ensembles,), (float(rank) if alpha is None else alpha) / rank, device=dev)
-            self.banks, self.w, self.bias, self.acts, self.grads_in, self.t = [], [], [], [], [], []
+            self.banks, self.w, self.bias, self.acts, self.t = [], [], [], [], []
             self.down, self.up, self.ddown, self.dup = [], [], [], []
             params, grads, copies = [], [], []
             for l in range(layers):
@@ -94,10 +94,14 @@ class AdapterTrainer:
                         copies.append(None)
                         use.append(view)
                 self.t.append(torch.zeros(batch, rank, device=dev))
-                # activations and their gradients: what the next layer reads, in its type
+                # activations: what the next layer reads, in its type
                 self.acts.append(_padded((batch, n_out), torch.float32 if l == layers - 1 else op, dev)[1])
-                self.grads_in.append(_padded((batch, n_out), lt, dev)[1])
+            # gradients of the output, of the activations, and the first layer's in its own type
+            self.dy = _padded((batch, self.widths[-1]), lt, dev)[1]
             self.dx = [None] + [_padded((batch, self.widths[l]), op, dev)[1] for l in range(1, layers)]
+            self.dy_first = None
+            if layers > 1 and op != torch.float32:
+                self.dy_first = _padded((batch, self.widths[1]), torch.float32, dev)[1]
             self.params, self.grads = params, grads
             self.m = [torch.zeros_like(p) for p in params]
             self.v = [torch.zeros_like(p) for p in params]
@@ -162,7 +166,7 @@ class AdapterTrainer:
             r = y - u
             self.loss.copy_((r * r).mean())
             last = self.n_layers - 1
-            dy = self.grads_in[last][:n]
+            dy = self.dy[:n]
             dy.copy_(r * (2.0 / r.numel()))
             for l in range(last, -1, -1):
                 inp = x if l == 0 else self.acts[l - 1][:n]
@@ -171,8 +175,8 @@ class AdapterTrainer:
                                        self.ddown[l], self.dup[l], dx=dx, scale=self.scale, relu_input=l > 0)
                 if l > 0:
                     dy = dx
-                    if l == 1 and dx.dtype != self.grads_in[0].dtype:     # the first layer computes in fp32
-                        dy = self.grads_in[0][:n]
+                    if l == 1 and self.dy_first is not None:              # the first layer computes in fp32
+                        dy = self.dy_first[:n]
                         dy.copy_(dx)
             self.adam.step(self.max_norm, self.norm)
 

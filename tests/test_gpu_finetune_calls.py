@@ -46,3 +46,22 @@ def test_numbers_of_rows(tuner):
         tuner.train_step(*rows(n))
     torch.cuda.synchronize()
     assert tuner.adam.get_steps() == 2 and bool(torch.isfinite(tuner.loss).all())
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_a_trainer_holds_the_arrays_that_a_step_needs(precision):
+    """Per hidden layer one array of activations and one of their gradients for the batch; per output its values and
+    their gradient; weights, adapters, gradients and moments (a quarter above their sum for paddings and the rest)."""
+    from paper_2309_16743_amd import OT_BF16, OT_FP32, Surrogate
+    from paper_2309_16743_amd.finetune import AdapterTrainer
+    widths, batch, e = (6, 16, 100_000, 16, 8), 1000, 2 if precision == "bf16" else 4
+    sur = Surrogate(widths, seed=3, max_batch=8)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    t = AdapterTrainer(sur, n_ensembles=2, rank=3, batch=batch, precision=OT_BF16 if e == 2 else OT_FP32)
+    held = torch.cuda.memory_allocated() - before
+    hidden = sum(2 * e * batch * w for w in widths[1:-1])
+    rest = sum(e * i * o + 2 * 3 * (i + o) * (16 + (2 if e == 2 else 0)) for i, o in zip(widths, widths[1:]))
+    assert held < 1.25 * (hidden + rest) + (4 << 20)
+    t.close()
+    sur.close()
