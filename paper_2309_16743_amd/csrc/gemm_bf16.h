@@ -1111,8 +1111,8 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
         for (int h = 0; h < FN; ++h) b[kk][h].template read<BK>(sb, BN / 8, WN * wn + 32 * h, kk, lane);
       }
     };
-    auto landed = [&](FragA (&a)[KK][FM], FragB (&b)[KK][FN]) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    auto wait = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    auto landed = [&](FragA (&a)[KK][FM], FragB (&b)[KK][FN]) {      // after wait()
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
 #pragma unroll
@@ -1137,12 +1137,14 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
           for (int h = 0; h < FN; ++h)
             acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[kk][f].get(), b[kk][h].get(), acc[f][h], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
+      wait();                                          // on every path, also after the last tile: no read passes it
       if (more) landed(an, bn);
     };
     if (nk > 0) {
       tile_ready(0);
       if (S - 1 < nk) issue(S - 1, S - 1);
       load_tile(0, a0, b0);
+      wait();
       landed(a0, b0);
     }
     for (int kt = 0; kt < nk; kt += 2) {
