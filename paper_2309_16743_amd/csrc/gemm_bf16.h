@@ -927,11 +927,14 @@ __device__ __forceinline__ bool adapt_lowrank(const GemmBArgs& g, Acc (&acc)[FM]
         hi = src[1];
       }
       float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      float big = 0.f;                                   // the largest, or NaN
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool bad = !(fabsf(x[e]) <= kBf16Max);
-        odd |= bad;
-        x[e] = bad ? 0.f : x[e];
+      for (int e = 0; e < 8; e += 2)
+        big = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(x[e]), fabsf(x[e + 1])), big);
+      if (__ballot(!(big <= kBf16Max)) != 0) {           // rare
+        odd = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fabsf(x[e]) <= kBf16Max ? x[e] : 0.f;
       }
       lr_split8(x, ts[f]);
     }
