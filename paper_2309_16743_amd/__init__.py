@@ -9,12 +9,13 @@ first call loads the library and raises if it was not built.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 from typing import Optional
 
 import numpy as np
 
 from . import _abi
-from ._abi import (OT_ADAPTERS_RELU, OT_ADAPTERS_RELU_INPUT, OT_BF16, OT_E_CLOSED, OT_E_INVAL, OT_E_STATE, OT_EMPTY, OT_FP32, OT_NOT_READY, OT_OK,
+from ._abi import (OT_ACT_GELU, OT_ACT_NONE, OT_ACT_RELU, OT_ACT_SILU, OT_ADAPTERS_RELU, OT_ADAPTERS_RELU_INPUT, OT_BF16, OT_E_CLOSED, OT_E_INVAL, OT_E_STATE, OT_EMPTY, OT_FP32, OT_NOT_READY, OT_OK,
                    OT_POLICY_FIFO, OT_POLICY_FIRO, OT_POLICY_RESERVOIR, OT_SURROGATE_KEEP_GRADS, OTError,
                    check, last_error, load)
 
@@ -27,7 +28,10 @@ __all__ = [
     "reservoir_checkpoint", "reservoir_restore", "surrogate_destroy", "LowRankAdapters", "GradientClip", "AdamTensors",
     "adapters_create", "adapters_forward", "adapters_backward", "adapters_destroy", "clip_create", "clip_norm",
     "clip_apply", "clip_destroy", "adam_create", "adam_step", "adam_set_lr", "adam_get_steps", "adam_set_steps",
-    "adam_destroy", "OT_ADAPTERS_RELU", "OT_ADAPTERS_RELU_INPUT", "load", "last_error", "OTError",
+    "adam_destroy", "DenseLayer", "GroupNorm", "Dropout", "dense_create", "dense_forward", "dense_backward",
+    "dense_destroy", "norm_create", "norm_forward", "norm_backward", "norm_destroy", "dropout_create",
+    "dropout_forward", "dropout_backward", "dropout_destroy", "OT_ACT_NONE", "OT_ACT_RELU", "OT_ACT_SILU",
+    "OT_ACT_GELU", "OT_ADAPTERS_RELU", "OT_ADAPTERS_RELU_INPUT", "load", "last_error", "OTError",
     "OT_OK", "OT_NOT_READY", "OT_EMPTY", "OT_E_INVAL", "OT_E_CLOSED", "OT_E_STATE", "OT_FP32", "OT_BF16",
     "OT_SURROGATE_KEEP_GRADS", "OT_POLICY_RESERVOIR", "OT_POLICY_FIFO", "OT_POLICY_FIRO",
 ]
@@ -324,7 +328,7 @@ def _matrix(t, rows: int, cols: int, dtype, device: int, what: str):
     return t.data_ptr(), st[0] if rows > 1 else max(st[0], cols)
 
 
-def _bank(t, n: int, rank: int, cols: int, dtype, device: int, what: str):
+def _bank(t, n: int, rank: int, cols: int, dtype, device: int, what: str, of: str = "adapters"):
     """(pointer, leading dimension) of an n x rank x cols tensor on the device whose rows follow each other."""
     shape, st = t.shape, t.stride()
     if t.dtype is not dtype or len(shape) != 3 or shape[0] != n or shape[1] != rank or shape[2] != cols or (
@@ -332,7 +336,7 @@ def _bank(t, n: int, rank: int, cols: int, dtype, device: int, what: str):
         raise ValueError(f"{what}: expected a {n} x {rank} x {cols} {dtype} tensor with unit column stride")
     ld = st[1] if rank > 1 else st[0] if n > 1 else max(st[0], cols)
     if n > 1 and st[0] != rank * ld:
-        raise ValueError(f"{what}: the rows of successive adapters must follow each other")
+        raise ValueError(f"{what}: the rows of successive {of} must follow each other")
     if t.get_device() != device:
         raise ValueError(f"{what}: expected a tensor on cuda:{device}")
     return t.data_ptr(), ld
@@ -565,6 +569,179 @@ class AdamTensors:
             pass
 
 
+class _Layer:
+    """What the layers' objects share: handle, device, closing."""
+    _destroy = ""
+
+    def _open(self, create: str, *args, precision: int) -> None:
+        import torch
+        h = C.c_void_p()
+        check(create, getattr(load(), create)(C.byref(h), *args))
+        self._h = h
+        self._torch, self._lib, self._device = torch, load(), torch.cuda.current_device()
+        self.precision = precision
+        self.dtype = torch.bfloat16 if precision == OT_BF16 else torch.float32
+
+    @property
+    def handle(self):
+        return self._h
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            check(self._destroy, getattr(load(), self._destroy)(self._h))
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class DenseLayer(_Layer):
+    """A dense layer y = act(x w^T + bias) + residual and its gradients (include/layers.h).
+    Tensors: x (n, in), w (out, in), bias fp32 (out); y and residual (n, out), float32 or bfloat16
+    alike; pre, dy (n, out); dx (n, in); dw fp32 (out, in); dbias fp32 (out).  activation:
+    OT_ACT_*.  max_rows: rows of the largest backward (0: a layer that only serves)."""
+    _destroy = "dense_destroy"
+
+    def __init__(self, in_dim: int, out_dim: int, precision: int = OT_FP32, activation: int = OT_ACT_NONE,
+                 max_rows: int = 1024):
+        self._open("dense_create", in_dim, out_dim, precision, activation, max_rows, precision=precision)
+        self.in_dim, self.out_dim, self.activation = in_dim, out_dim, activation
+
+    def forward(self, x, w, y, bias=None, residual=None, pre=None, stream=None) -> None:
+        """y = act(x w^T + bias) + residual; pre receives x w^T + bias for backward().  y may be the residual."""
+        torch, dev = self._torch, self._device
+        n = x.shape[0]
+        xp = _matrix(x, n, self.in_dim, self.dtype, dev, "x")
+        wp = _matrix(w, self.out_dim, self.in_dim, self.dtype, dev, "w")
+        y_type = y.dtype
+        if y_type is not torch.float32 and y_type is not torch.bfloat16:
+            raise ValueError("y: expected float32 or bfloat16")
+        yp = _matrix(y, n, self.out_dim, y_type, dev, "y")
+        rp = (None, 0) if residual is None else _matrix(residual, n, self.out_dim, y_type, dev, "residual")
+        pp = (None, 0) if pre is None else _matrix(pre, n, self.out_dim, self.dtype, dev, "pre")
+        check("dense_forward", self._lib.dense_forward(
+            self._h, *xp, *wp, _vector(bias, self.out_dim, torch.float32, dev, "bias"), *rp, n, *yp,
+            OT_BF16 if y_type is torch.bfloat16 else OT_FP32, *pp, _raw_stream(stream, dev, torch)))
+
+    def backward(self, x, w, dy, pre=None, dx=None, dw=None, dbias=None, stream=None) -> None:
+        """Gradients from dy (and pre, where the layer has an activation), written whole into those of dx, dw, dbias
+        that are given; x may be None without dw, w without dx."""
+        torch, dev = self._torch, self._device
+        n = dy.shape[0]
+        if dw is not None and x is None:
+            raise ValueError("dw needs x")
+        if dx is not None and w is None:
+            raise ValueError("dx needs w")
+        if pre is None and self.activation != OT_ACT_NONE:
+            raise ValueError("pre: expected what forward() stored")
+        none = (None, 0)
+        xp = none if x is None else _matrix(x, n, self.in_dim, self.dtype, dev, "x")
+        wp = none if w is None else _matrix(w, self.out_dim, self.in_dim, self.dtype, dev, "w")
+        dyp = _matrix(dy, n, self.out_dim, self.dtype, dev, "dy")
+        pp = none if pre is None else _matrix(pre, n, self.out_dim, self.dtype, dev, "pre")
+        dxp = none if dx is None else _matrix(dx, n, self.in_dim, self.dtype, dev, "dx")
+        dwp = none if dw is None else _matrix(dw, self.out_dim, self.in_dim, torch.float32, dev, "dw")
+        check("dense_backward", self._lib.dense_backward(
+            self._h, *xp, *wp, n, *dyp, *pp, *dxp, *dwp, _vector(dbias, self.out_dim, torch.float32, dev, "dbias"),
+            _raw_stream(stream, dev, torch)))
+
+
+class GroupNorm(_Layer):
+    """Group norm with an activation over channels-last data (include/layers.h).  x, y, dy and dx are
+    (samples, positions, channels), or (samples, channels) with one position; weight, bias, dweight and
+    dbias fp32 (channels); stats fp32 (samples, groups, 2).  activation: OT_ACT_*."""
+    _destroy = "norm_destroy"
+
+    def __init__(self, channels: int, groups: int, positions: int = 1, precision: int = OT_FP32,
+                 activation: int = OT_ACT_NONE, eps: float = 1e-5, max_samples: int = 1024):
+        self._open("norm_create", channels, groups, positions, precision, activation, eps, max_samples,
+                   precision=precision)
+        self.channels, self.groups, self.positions, self.activation = channels, groups, positions, activation
+
+    def _rows(self, t, n: int, what: str):
+        """(pointer, leading dimension) of the rows of n samples."""
+        shape = t.shape
+        if len(shape) == 2 and self.positions == 1:
+            return _matrix(t, n, self.channels, self.dtype, self._device, what)
+        return _bank(t, n, self.positions, self.channels, self.dtype, self._device, what, "samples")
+
+    def _stats(self, t, n: int):
+        if t is None:
+            return None
+        if t.dtype is not self._torch.float32 or tuple(t.shape) != (n, self.groups, 2) or not t.is_contiguous():
+            raise ValueError(f"stats: expected a contiguous torch.float32 tensor of {n} x {self.groups} x 2 values")
+        if t.get_device() != self._device:
+            raise ValueError(f"stats: expected a tensor on cuda:{self._device}")
+        return t.data_ptr()
+
+    def forward(self, x, y, weight=None, bias=None, stats=None, stream=None) -> None:
+        """y = act(weight (x - mean) rstd + bias); stats receives mean and rstd for backward().  y may be x."""
+        torch, dev, c = self._torch, self._device, self.channels
+        n = x.shape[0]
+        check("norm_forward", self._lib.norm_forward(
+            self._h, *self._rows(x, n, "x"), _vector(weight, c, torch.float32, dev, "weight"),
+            _vector(bias, c, torch.float32, dev, "bias"), n, *self._rows(y, n, "y"), self._stats(stats, n),
+            _raw_stream(stream, dev, torch)))
+
+    def backward(self, x, stats, dy, weight=None, bias=None, dx=None, dweight=None, dbias=None, stream=None) -> None:
+        """Gradients from dy and the forward's stats, written whole into those of dx, dweight, dbias that are
+        given.  dx may be dy."""
+        torch, dev, c = self._torch, self._device, self.channels
+        n = x.shape[0]
+        check("norm_backward", self._lib.norm_backward(
+            self._h, *self._rows(x, n, "x"), _vector(weight, c, torch.float32, dev, "weight"),
+            _vector(bias, c, torch.float32, dev, "bias"), n, self._stats(stats, n), *self._rows(dy, n, "dy"),
+            *((None, 0) if dx is None else self._rows(dx, n, "dx")), _vector(dweight, c, torch.float32, dev, "dweight"),
+            _vector(dbias, c, torch.float32, dev, "dbias"), _raw_stream(stream, dev, torch)))
+
+
+class Dropout(_Layer):
+    """Dropout whose mask comes from a counter (seed, site, step, row, column) and is never stored
+    (include/layers.h).  x, residual, y, dy, dx: (rows, columns).  step: an int, or a device int64 tensor of
+    one element, read when the kernel runs (so that replays of a captured call take masks of
+    their own)."""
+    _destroy = "dropout_destroy"
+
+    def __init__(self, p: float, seed: int, site: int = 0, precision: int = OT_FP32):
+        if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 32:
+            raise ValueError("seed: expected a value of 64 bits, site: one of 32")
+        self._open("dropout_create", p, seed, site, precision, precision=precision)
+        self.p, self.seed, self.site = p, seed, site
+
+    def _step(self, step):
+        """(host part, device part)."""
+        if not hasattr(step, "data_ptr"):
+            step = operator.index(step)
+            if not 0 <= step < 1 << 32:
+                raise ValueError("step: expected a value of 32 bits")
+            return step, None
+        if step.dtype is not self._torch.int64 or step.numel() != 1:
+            raise ValueError("step: expected an int or an int64 tensor of one element")
+        if step.get_device() != self._device:
+            raise ValueError(f"step: expected a tensor on cuda:{self._device}")
+        return 0, step.data_ptr()
+
+    def forward(self, x, y, step, residual=None, stream=None) -> None:
+        """y = residual + (x / (1 - p) where it is kept).  y may be x or the residual."""
+        n, cols = x.shape
+        dev = self._device
+        xp, yp = _matrix(x, n, cols, self.dtype, dev, "x"), _matrix(y, n, cols, self.dtype, dev, "y")
+        rp = (None, 0) if residual is None else _matrix(residual, n, cols, self.dtype, dev, "residual")
+        check("dropout_forward", self._lib.dropout_forward(self._h, *xp, *rp, n, cols, *yp, *self._step(step),
+                                                           _raw_stream(stream, dev, self._torch)))
+
+    def backward(self, dy, dx, step, stream=None) -> None:
+        """dx = dy / (1 - p) where forward() of the same step kept x.  dx may be dy."""
+        n, cols = dy.shape
+        dev = self._device
+        dyp, dxp = _matrix(dy, n, cols, self.dtype, dev, "dy"), _matrix(dx, n, cols, self.dtype, dev, "dx")
+        check("dropout_backward", self._lib.dropout_backward(self._h, *dyp, n, cols, *dxp, *self._step(step),
+                                                             _raw_stream(stream, dev, self._torch)))
+
+
 # ---- C-named entry points (argument marshalling only) ----------------------------
 def reservoir_create(capacity, threshold, x_dim, u_dim, seed, policy=OT_POLICY_RESERVOIR,
                      order_stream=None) -> Reservoir:
@@ -717,3 +894,53 @@ def adam_set_steps(a: AdamTensors, steps) -> None:
 
 def adam_destroy(a: AdamTensors) -> None:
     a.close()
+
+
+def dense_create(in_dim, out_dim, precision=OT_FP32, activation=OT_ACT_NONE, max_rows=1024) -> DenseLayer:
+    return DenseLayer(in_dim, out_dim, precision, activation, max_rows)
+
+
+def dense_forward(d: DenseLayer, x, w, y, bias=None, residual=None, pre=None, stream=None) -> None:
+    d.forward(x, w, y, bias, residual, pre, stream)
+
+
+def dense_backward(d: DenseLayer, x, w, dy, pre=None, dx=None, dw=None, dbias=None, stream=None) -> None:
+    d.backward(x, w, dy, pre, dx, dw, dbias, stream)
+
+
+def dense_destroy(d: DenseLayer) -> None:
+    d.close()
+
+
+def norm_create(channels, groups, positions=1, precision=OT_FP32, activation=OT_ACT_NONE, eps=1e-5,
+                max_samples=1024) -> GroupNorm:
+    return GroupNorm(channels, groups, positions, precision, activation, eps, max_samples)
+
+
+def norm_forward(d: GroupNorm, x, y, weight=None, bias=None, stats=None, stream=None) -> None:
+    d.forward(x, y, weight, bias, stats, stream)
+
+
+def norm_backward(d: GroupNorm, x, stats, dy, weight=None, bias=None, dx=None, dweight=None, dbias=None,
+                  stream=None) -> None:
+    d.backward(x, stats, dy, weight, bias, dx, dweight, dbias, stream)
+
+
+def norm_destroy(d: GroupNorm) -> None:
+    d.close()
+
+
+def dropout_create(p, seed, site=0, precision=OT_FP32) -> Dropout:
+    return Dropout(p, seed, site, precision)
+
+
+def dropout_forward(d: Dropout, x, y, step, residual=None, stream=None) -> None:
+    d.forward(x, y, step, residual, stream)
+
+
+def dropout_backward(d: Dropout, dy, dx, step, stream=None) -> None:
+    d.backward(dy, dx, step, stream)
+
+
+def dropout_destroy(d: Dropout) -> None:
+    d.close()

@@ -1,5 +1,5 @@
 """ctypes declarations of the C ABI (include/ot_status.h, reservoir.h, surrogate.h, adapters.h,
-gradients.h).
+gradients.h, layers.h).
 
 Argument marshalling only.  Loading fails loudly when the library has not been
 built: there is no fallback implementation.
@@ -25,6 +25,10 @@ OT_BF16 = 1
 OT_SURROGATE_KEEP_GRADS = 1
 OT_ADAPTERS_RELU = 1
 OT_ADAPTERS_RELU_INPUT = 2
+OT_ACT_NONE = 0
+OT_ACT_RELU = 1
+OT_ACT_SILU = 2
+OT_ACT_GELU = 3
 OT_POLICY_RESERVOIR = 0
 OT_POLICY_FIFO = 1
 OT_POLICY_FIRO = 2
@@ -48,6 +52,7 @@ i32 = C.c_int32
 u64 = C.c_uint64
 u32 = C.c_uint32
 f32 = C.c_float
+f64 = C.c_double
 
 SIGNATURES = {
     "ot_last_error": (C.c_char_p, []),
@@ -100,6 +105,18 @@ SIGNATURES = {
     "adam_get_steps": (C.c_int, [vp, C.POINTER(i64)]),
     "adam_set_steps": (C.c_int, [vp, i64]),
     "adam_destroy": (C.c_int, [vp]),
+    "dense_create": (C.c_int, [C.POINTER(vp), i64, i64, i32, i32, i64]),
+    "dense_forward": (C.c_int, [vp, vp, i64, vp, i64, vp, vp, i64, i64, vp, i64, i32, vp, i64, vp]),
+    "dense_backward": (C.c_int, [vp, vp, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]),
+    "dense_destroy": (C.c_int, [vp]),
+    "norm_create": (C.c_int, [C.POINTER(vp), i64, i32, i64, i32, i32, f32, i64]),
+    "norm_forward": (C.c_int, [vp, vp, i64, vp, vp, i64, vp, i64, vp, vp]),
+    "norm_backward": (C.c_int, [vp, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp]),
+    "norm_destroy": (C.c_int, [vp]),
+    "dropout_create": (C.c_int, [C.POINTER(vp), f64, u64, u32, i32]),
+    "dropout_forward": (C.c_int, [vp, vp, i64, vp, i64, i64, i64, vp, i64, i64, vp, vp]),
+    "dropout_backward": (C.c_int, [vp, vp, i64, i64, i64, vp, i64, i64, vp, vp]),
+    "dropout_destroy": (C.c_int, [vp]),
 }
 
 _lib = None

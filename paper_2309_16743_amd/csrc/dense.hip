@@ -1,0 +1,264 @@
+// Dense layer with bias, activation and residual (include/layers.h): entry points, the
+// activation's backward and the column sums.  The products are in dense_bf16.hip and dense_f32.hip.
+#include <cmath>
+#include <new>
+
+#include "dense_products.h"
+#include "layer_host.h"
+#include "layer_plan.h"
+#include "layers.h"
+#include "row_ops.h"
+#include "surrogate.h"
+
+namespace ot {
+
+struct SlopeArgs {
+  const void* dy;
+  int64_t lddy;
+  const void* pre;          // nullable: dz = dy
+  int64_t ldp;
+  void* dz;                 // rows of lddz values, planes plane_stride elements apart
+  int64_t lddz, plane_stride;
+  int64_t n, cols;
+  int32_t act;
+  float* sums;              // [chunk][cols] (nullable)
+  ColumnPlan plan;
+};
+
+// dz = dy act'(pre) and its column sums.  PLANES: what is written of dz (0: nothing, dz is dy): one matrix, or in
+// bf16 the three terms whose sum is dz in 24 bits.
+template <class T, int PLANES>
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
+  __shared__ float s[256][9];
+  const int w = a.plan.col_threads, cx = threadIdx.x % w, rx = threadIdx.x / w, lanes = 256 / w;
+  const int64_t c = ((int64_t)blockIdx.x * w + cx) * 8;
+  const int64_t r0 = (int64_t)blockIdx.y * a.plan.rows, r1 = min(a.n, r0 + a.plan.rows);
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (c < a.cols) {
+#pragma unroll 2
+    for (int64_t r = r0 + rx; r < r1; r += lanes) {
+      float v[8];
+      load8(static_cast<const T*>(a.dy) + r * a.lddy + c, a.cols - c, v);
+      if constexpr (PLANES > 0) {
+        float z[8];
+        load8(static_cast<const T*>(a.pre) + r * a.ldp + c, a.cols - c, z);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_back(v[e], z[e], a.act);
+        T* out = static_cast<T*>(a.dz) + r * a.lddz + c;
+        if constexpr (PLANES == 3) {
+          lr_u32x4 t[3];
+          lr_split8(v, t);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) *reinterpret_cast<lr_u32x4*>(out + p * a.plane_stride) = t[p];
+        } else {
+          store8(out, 8, v);                             // (rows of dz are padded to 8 values)
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    }
+  }
+  if (!a.sums) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[threadIdx.x][e] = sum[e];
+  for (int h = lanes / 2; h > 0; h /= 2) {
+    __syncthreads();
+    if (rx < h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[threadIdx.x][e] += s[threadIdx.x + h * w][e];
+  }
+  if (rx == 0)
+    for (int e = 0; e < 8; ++e)
+      if (c + e < a.cols) a.sums[blockIdx.y * a.cols + c + e] = s[threadIdx.x][e];
+}
+
+// Sums of the chunks' partials in a fixed order: a block takes 64 columns, its 16 wavefronts each a
+// sixteenth of the chunks.
+__global__ __launch_bounds__(1024) void column_join_kernel(const float* __restrict__ part, int64_t chunks, int64_t cols,
+                                                           float* __restrict__ out) {
+  __shared__ float s[16][64];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  float sum = 0.f;
+  if (c < cols)
+#pragma unroll 8
+    for (int64_t k = wid; k < chunks; k += 16) sum += part[k * cols + c];
+  s[wid][lane] = sum;
+  __syncthreads();
+  if (wid == 0 && c < cols) {
+    for (int k = 1; k < 16; ++k) sum += s[k][lane];
+    out[c] = sum;
+  }
+}
+
+__global__ __launch_bounds__(256) void zero_rows_kernel(float* p, int64_t ld, int64_t rows, int64_t cols) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  for (int64_t k = i; k < rows * cols; k += step) p[k / cols * ld + k % cols] = 0.f;
+}
+
+}  // namespace ot
+
+struct ot_dense {
+  int64_t in, out;
+  int32_t precision, act;
+  int device;
+  ot::Workspace ws;
+  ot::DenseSizes sizes() const {
+    const bool bf16 = precision == OT_BF16;
+    const int32_t planes = act == OT_ACT_NONE ? 0 : bf16 && act != OT_ACT_RELU ? 3 : 1;
+    return {in, out, bf16, planes};
+  }
+  int64_t bytes(int64_t n) const { return n < 1 ? 0 : ot::dz_bytes(sizes(), n) + 4 * ot::dense_values(sizes(), n); }
+};
+
+namespace {
+
+constexpr int64_t kMost = 1LL << 26, kMostValues = 1LL << 36;
+
+int run_product(ot::Product p, const ot_dense* d, const ot::ProductArgs& a, hipStream_t st) {
+  return d->precision == OT_BF16 ? ot::run_product_bf16(p, a, st) : ot::run_product_f32(p, a, st);
+}
+
+int run_slope(const ot_dense* d, ot::SlopeArgs a, int planes, float* dbias, float* part, hipStream_t st) {
+  a.plan = ot::plan_columns(a.n, a.cols);
+  a.sums = dbias ? (a.plan.chunks > 1 ? part : dbias) : nullptr;
+  const dim3 grid((unsigned)a.plan.blocks_x, (unsigned)a.plan.chunks), block(256);
+  if (d->precision == OT_FP32) {
+    if (planes) hipLaunchKernelGGL((ot::slope_kernel<float, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((ot::slope_kernel<float, 0>), grid, block, 0, st, a);
+  } else {
+    if (planes == 3) hipLaunchKernelGGL((ot::slope_kernel<uint16_t, 3>), grid, block, 0, st, a);
+    else if (planes) hipLaunchKernelGGL((ot::slope_kernel<uint16_t, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((ot::slope_kernel<uint16_t, 0>), grid, block, 0, st, a);
+  }
+  OT_LAUNCHED("slope_kernel");
+  if (dbias && a.plan.chunks > 1) {
+    hipLaunchKernelGGL(ot::column_join_kernel, dim3((unsigned)ot::ceil_div(a.cols, 64)), dim3(1024), 0, st, part,
+                       a.plan.chunks, a.cols, dbias);
+    OT_LAUNCHED("column_join_kernel");
+  }
+  return OT_OK;
+}
+
+int zero_rows(float* p, int64_t ld, int64_t rows, int64_t cols, hipStream_t st) {
+  const int64_t blocks = std::min<int64_t>(4096, ot::ceil_div(rows * cols, 256));
+  hipLaunchKernelGGL(ot::zero_rows_kernel, dim3((unsigned)blocks), dim3(256), 0, st, p, ld, rows, cols);
+  OT_LAUNCHED("zero_rows_kernel");
+  return OT_OK;
+}
+
+}  // namespace
+
+extern "C" int dense_create(ot_dense** out, int64_t in, int64_t out_dim, int32_t precision, int32_t activation,
+                            int64_t max_rows) {
+  ot::clear_error();
+  OT_REQUIRE(out != nullptr, "dense_create: NULL out");
+  *out = nullptr;
+  OT_REQUIRE(in >= 1 && in <= kMost && out_dim >= 1 && out_dim <= kMost, "dense_create: in or out outside [1, 2^26]");
+  OT_REQUIRE(in * out_dim <= kMostValues, "dense_create: more than 2^36 weights");
+  OT_REQUIRE(precision == OT_FP32 || precision == OT_BF16, "dense_create: unknown precision");
+  OT_REQUIRE(activation >= OT_ACT_NONE && activation <= OT_ACT_GELU, "dense_create: unknown activation");
+  OT_REQUIRE(max_rows >= 0 && max_rows <= kMost, "dense_create: max_rows outside [0, 2^26]");
+  OT_REQUIRE(max_rows * std::max(in, out_dim) <= kMostValues, "dense_create: more than 2^36 values in max_rows rows");
+  int device = -1;
+  OT_HIP(hipGetDevice(&device));
+  ot_dense* d = new (std::nothrow) ot_dense();
+  if (!d) return ot::set_error(OT_E_NOMEM, "dense_create: out of host memory");
+  d->in = in;
+  d->out = out_dim;
+  d->precision = precision;
+  d->act = activation;
+  d->device = device;
+  const int rc = d->ws.allocate(max_rows, d->bytes(max_rows), "dense_create");
+  if (rc) {
+    delete d;
+    return rc;
+  }
+  *out = d;
+  return OT_OK;
+}
+
+extern "C" int dense_forward(ot_dense* d, const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias,
+                             const void* residual, int64_t ldr, int64_t n, void* y, int64_t ldy, int32_t y_type,
+                             void* pre, int64_t ldp, void* stream) {
+  ot::clear_error();
+  const char* what = "dense_forward";
+  OT_REQUIRE(d != nullptr, "%s: NULL layer", what);
+  OT_REQUIRE(n >= 0 && n <= kMost, "%s: n outside [0, 2^26]", what);
+  OT_REQUIRE(n * std::max(d->in, d->out) <= kMostValues, "%s: more than 2^36 values", what);
+  OT_REQUIRE(y_type == OT_FP32 || y_type == OT_BF16, "%s: y_type is neither OT_FP32 nor OT_BF16", what);
+  if (n == 0) return OT_OK;
+  const int e = d->precision == OT_BF16 ? 2 : 4, ey = y_type == OT_BF16 ? 2 : 4;
+  int rc;
+  if ((rc = ot::check_rows(x, ldx, n, d->in, e, what, "x"))) return rc;
+  if ((rc = ot::check_rows(w, ldw, d->out, d->in, e, what, "w"))) return rc;
+  if ((rc = ot::check_rows(y, ldy, n, d->out, ey, what, "y"))) return rc;
+  if (residual && (rc = ot::check_rows(residual, ldr, n, d->out, ey, what, "residual"))) return rc;
+  if (pre && (rc = ot::check_rows(pre, ldp, n, d->out, e, what, "pre"))) return rc;
+  if ((rc = ot::check_values(bias, 4, what, "bias"))) return rc;
+  if ((rc = ot::check_device(d->device, what))) return rc;
+  const ot::ProductArgs a{x, ldx, w, ldw, n, d->out, d->in, bias, y, ldy, y_type,
+                          ot::LayerArgs{residual, ldr, pre, ldp, d->act, 1, 0}, nullptr};
+  return run_product(ot::Product::Forward, d, a, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int dense_backward(ot_dense* d, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n,
+                              const void* dy, int64_t lddy, const void* pre, int64_t ldp, void* dx, int64_t lddx,
+                              float* dw, int64_t lddw, float* dbias, void* stream) try {
+  ot::clear_error();
+  const char* what = "dense_backward";
+  OT_REQUIRE(d != nullptr, "%s: NULL layer", what);
+  OT_REQUIRE(n >= 0 && n <= kMost, "%s: n outside [0, 2^26]", what);
+  OT_REQUIRE(n * std::max(d->in, d->out) <= kMostValues, "%s: more than 2^36 values", what);
+  const int e = d->precision == OT_BF16 ? 2 : 4;
+  const ot::DenseSizes sz = d->sizes();
+  int rc;
+  if (dw && (rc = ot::check_rows(dw, lddw, d->out, d->in, 4, what, "dw"))) return rc;
+  if ((rc = ot::check_values(dbias, 4, what, "dbias"))) return rc;
+  if (n > 0) {
+    if ((rc = ot::check_rows(dy, lddy, n, d->out, e, what, "dy"))) return rc;
+    if (sz.planes && (rc = ot::check_rows(pre, ldp, n, d->out, e, what, "pre"))) return rc;
+    if (dw && (rc = ot::check_rows(x, ldx, n, d->in, e, what, "x"))) return rc;
+    if (dx) {
+      if ((rc = ot::check_rows(w, ldw, d->out, d->in, e, what, "w"))) return rc;
+      if ((rc = ot::check_rows(dx, lddx, n, d->in, e, what, "dx"))) return rc;
+    }
+  }
+  if ((rc = ot::check_device(d->device, what))) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (n == 0) {
+    if (dw && (rc = zero_rows(dw, lddw, d->out, d->in, st))) return rc;
+    return dbias ? zero_rows(dbias, d->out, 1, d->out, st) : OT_OK;
+  }
+  if (!dx && !dw && !dbias) return OT_OK;
+  if ((rc = d->ws.begin(n, st, what, [&](int64_t rows) { return d->bytes(rows); }))) return rc;
+  const int64_t ldz = sz.planes ? ot::dz_ld(sz) : lddy;
+  void* dz = sz.planes ? d->ws.p : const_cast<void*>(dy);
+  float* part = reinterpret_cast<float*>(d->ws.p + ot::dz_bytes(sz, n));
+  if (sz.planes || dbias) {
+    const ot::SlopeArgs s{dy, lddy, pre, ldp, dz, ldz, n * ldz, n, d->out, d->act, nullptr, {}};
+    if ((rc = run_slope(d, s, sz.planes, dbias, part, st))) return rc;
+  }
+  ot::LayerArgs ly{};
+  ly.planes = std::max(1, sz.planes);
+  ly.plane_stride = n * ldz;
+  if (dw) {
+    const ot::ProductArgs a{dz, ldz, x, ldx, d->out, d->in, n, nullptr, dw, lddw, OT_FP32, ly, part};
+    if ((rc = run_product(ot::Product::WeightGrad, d, a, st))) return rc;
+  }
+  if (dx) {
+    const ot::ProductArgs a{dz, ldz, w, ldw, n, d->in, d->out, nullptr, dx, lddx, d->precision, ly, part};
+    if ((rc = run_product(ot::Product::InputGrad, d, a, st))) return rc;
+  }
+  return OT_OK;
+} catch (const std::bad_alloc&) {
+  return ot::set_error(OT_E_NOMEM, "dense_backward: out of host memory");
+}
+
+extern "C" int dense_destroy(ot_dense* d) {
+  ot::clear_error();
+  if (!d) return OT_OK;
+  d->ws.release();
+  delete d;
+  return OT_OK;
+}

@@ -1,0 +1,69 @@
+// Products of a bf16 dense layer: gemm_bf16.h's kernels with their Layer epilogues.
+#include "dense_products.h"
+#include "gemm_bf16.h"
+#include "layer_plan.h"
+#include "surrogate.h"
+
+namespace ot {
+namespace {
+
+constexpr LayB KM = LayB::KMajor, MN = LayB::MNMajor;
+
+// The tiles that the plans give for each product.
+template <LayB LA, LayB LB, EpiB E>
+hipError_t launch(int tile, const GemmBArgs& g, int64_t splits, hipStream_t st) {
+  if constexpr (LB == KM) {
+    if (tile == kB64x64) return launch_gemm_bf16_pipe<64, 64, 64, 4, 2, LA, LB, E>(g, splits, st);
+  }
+  if constexpr (LA == KM) {
+    if (tile == kB64x128) return launch_gemm_bf16_pipe<64, 128, 64, 3, 4, LA, LB, E, 4>(g, splits, st);
+  }
+  if (tile == kB128x128) return launch_gemm_bf16_pipe<128, 128, 32, 4, 2, LA, LB, E>(g, splits, st);
+  if constexpr (!(LA == MN && E == EpiB::LayerSplit)) {
+    if (tile == kB256x256) return launch_gemm_bf16_pp<4, LA, LB, E>(g, splits, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+int run_product_bf16(Product p, const ProductArgs& a, hipStream_t st) {
+  const AdaptPlan plan = p == Product::WeightGrad ? plan_wgrad(true, a.M, a.N, a.K)
+                                                  : plan_expand(true, p == Product::Forward, a.M, a.N, a.K);
+  GemmBArgs g{};
+  g.A = static_cast<const uint16_t*>(a.A);
+  g.lda = a.lda;
+  g.B = static_cast<const uint16_t*>(a.B);
+  g.ldb = a.ldb;
+  g.C = a.C;
+  g.ldc = a.ldc;
+  g.M = a.M;
+  g.N = a.N;
+  g.K = a.K;
+  g.k_chunk = plan.k_chunk;
+  g.bias = a.bias;
+  g.ly = a.ly;
+  const bool split = plan.splits > 1;
+  if (split) {
+    g.C = a.part;
+    g.ldc = (a.N + 3) / 4 * 4;
+    g.split_stride = a.M * g.ldc;
+  }
+  hipError_t rc;
+  if (p == Product::Forward)
+    rc = a.c_type == OT_BF16 ? launch<KM, KM, EpiB::LayerBf>(plan.tile, g, 1, st)
+                             : launch<KM, KM, EpiB::LayerF32>(plan.tile, g, 1, st);
+  else if (p == Product::InputGrad)
+    rc = split ? launch<KM, MN, EpiB::LayerSplit>(plan.tile, g, plan.splits, st)
+               : launch<KM, MN, EpiB::LayerBf>(plan.tile, g, 1, st);
+  else
+    rc = split ? launch<MN, MN, EpiB::LayerSplit>(plan.tile, g, plan.splits, st)
+               : launch<MN, MN, EpiB::LayerF32>(plan.tile, g, 1, st);
+  if (rc != hipSuccess)
+    return set_error(OT_E_HIP, "launch of the dense product failed: %s", hipGetErrorString(rc));
+  if (!split) return OT_OK;
+  return p == Product::InputGrad ? join_splits<uint16_t>(a, plan.splits, g.split_stride, g.ldc, st)
+                                 : join_splits<float>(a, plan.splits, g.split_stride, g.ldc, st);
+}
+
+}  // namespace ot

@@ -27,6 +27,7 @@
 
 #include "adam.h"
 #include "common.h"
+#include "layer_ops.h"
 #include "lowrank_ops.h"
 
 namespace ot {
@@ -65,9 +66,14 @@ enum class EpiB : int {
   // low-rank product (split 0), K may have any length
   AdaptF32 = 7,   // C (fp32) row perm[m] = acc (+ bias[n]) (ReLU)
   AdaptBf = 8,    // C (bf16) row perm[m] = bf16(acc (+ bias[n]) (ReLU, or 0 where lr.mask is not above 0))
-  AdaptSplit = 9  // C (fp32)[split] row m = acc
+  AdaptSplit = 9, // C (fp32)[split] row m = acc
+  // Dense layers (dense.hip): K may have any length, A may be the sum of several planes
+  LayerF32 = 10, // C (fp32) = act(acc (+ bias[n])) (+ ly.residual, fp32); ly.pre (bf16) = acc (+ bias[n])
+  LayerBf = 11,  // C (bf16) = bf16 of the same (residual bf16)
+  LayerSplit = 12 // C (fp32)[split] = acc
 };
 constexpr bool is_adapt(EpiB e) { return e == EpiB::AdaptF32 || e == EpiB::AdaptBf || e == EpiB::AdaptSplit; }
+constexpr bool is_layer(EpiB e) { return e == EpiB::LayerF32 || e == EpiB::LayerBf || e == EpiB::LayerSplit; }
 
 struct GemmBArgs {
   const uint16_t* A;
@@ -97,6 +103,7 @@ struct GemmBArgs {
   uint16_t* adam_pb;
   AdamArgs adam;
   AdaptRows lr;             // Adapt*
+  LayerArgs ly;             // Layer*
 };
 
 __device__ __forceinline__ int64_t xcd_remap_b(int64_t p, int64_t g) {
@@ -192,7 +199,8 @@ struct BEpi {
         for (int c = 0; c < 4; ++c) bias4[c] = (col + c < g.N) ? g.bias[col + c] : 0.f;
       }
     }
-    if constexpr (EPI == EpiB::AdaptF32 || EPI == EpiB::AdaptBf) {       // the caller's bias: any alignment
+    if constexpr (EPI == EpiB::AdaptF32 || EPI == EpiB::AdaptBf || EPI == EpiB::LayerF32 ||
+                  EPI == EpiB::LayerBf) {                // the caller's bias: any alignment
       if (g.bias)
         for (int c = 0; c < 4; ++c) bias4[c] = (col + c < g.N) ? g.bias[col + c] : 0.f;
     }
@@ -210,6 +218,10 @@ struct BEpi {
     }
     if constexpr (is_adapt(EPI)) {
       adapt_rows<NP>(g, ep, m0, split, stage);
+      return;
+    }
+    if constexpr (is_layer(EPI)) {
+      layer_rows<NP>(g, ep, m0, split, stage);
       return;
     }
     // targets (MseBf) or mask (MaskBf) of each pass; one branch around all
@@ -347,6 +359,80 @@ struct BEpi {
           else
             for (int c = 0; c < 4; ++c)
               if (col + c < g.N) C[c] = h[c];
+        }
+      }
+    }
+  }
+
+  // Layer*: the residuals of G passes are read together.  Rows are padded to whole 16-byte pieces,
+  // so 4 columns are read together if one exists; a lane reads its residuals before it writes the same
+  // columns of C, which may be the residual itself.
+  template <int NP, class Stage>
+  __device__ __forceinline__ void layer_rows(const GemmBArgs& g, const float* ep, int64_t m0, int64_t split,
+                                             Stage stage) {
+    constexpr int G = NP < 4 ? NP : 4;
+    static_assert(NP % G == 0, "pass groups");
+    stage();
+    if (col >= g.N) return;
+    if constexpr (EPI == EpiB::LayerSplit) {
+      float* C = reinterpret_cast<float*>(g.C) + split * g.split_stride + col;   // rows padded to whole vectors
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int64_t m = m0 + rl + RPP * i;
+        if (m < g.M)
+          *reinterpret_cast<f32x4*>(C + m * g.ldc) = *reinterpret_cast<const f32x4*>(ep + (rl + RPP * i) * EP + 4 * cg);
+      }
+      return;
+    }
+    const int cnt = (int)min((int64_t)4, g.N - col);
+#pragma unroll 1
+    for (int i0 = 0; i0 < NP; i0 += G) {
+      f32x4 res[G];
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        res[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int64_t m = min(m0 + rl + RPP * (i0 + u), g.M - 1);
+        if (g.ly.residual) {
+          if constexpr (EPI == EpiB::LayerF32) {
+            res[u] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(g.ly.residual) + m * g.ly.ldr + col);
+          } else {
+            const u16x4 h =
+                *reinterpret_cast<const u16x4*>(static_cast<const uint16_t*>(g.ly.residual) + m * g.ly.ldr + col);
+            res[u] = f32x4{bf2f(h[0]), bf2f(h[1]), bf2f(h[2]), bf2f(h[3])};
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        const int rr = rl + RPP * (i0 + u);
+        const int64_t m = m0 + rr;
+        if (m >= g.M) continue;
+        f32x4 v = *reinterpret_cast<const f32x4*>(ep + rr * EP + 4 * cg);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] += bias4[c];
+        if (g.ly.pre) {
+          uint16_t* P = static_cast<uint16_t*>(g.ly.pre) + m * g.ly.ldp + col;
+          const u16x4 h = {lr_bf16(v[0]), lr_bf16(v[1]), lr_bf16(v[2]), lr_bf16(v[3])};
+          if (cnt == 4) *reinterpret_cast<u16x4*>(P) = h;
+          else
+            for (int c = 0; c < cnt; ++c) P[c] = h[c];
+        }
+        if (g.ly.act != kActNone) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[c] = act_value(v[c], g.ly.act);
+        }
+        v += res[u];
+        if constexpr (EPI == EpiB::LayerF32) {
+          float* C = reinterpret_cast<float*>(g.C) + m * g.ldc + col;
+          if (cnt == 4) *reinterpret_cast<f32x4*>(C) = v;
+          else
+            for (int c = 0; c < cnt; ++c) C[c] = v[c];
+        } else {
+          uint16_t* C = reinterpret_cast<uint16_t*>(g.C) + m * g.ldc + col;
+          const u16x4 h = {lr_bf16(v[0]), lr_bf16(v[1]), lr_bf16(v[2]), lr_bf16(v[3])};
+          if (cnt == 4) *reinterpret_cast<u16x4*>(C) = h;
+          else
+            for (int c = 0; c < cnt; ++c) C[c] = h[c];
         }
       }
     }
@@ -890,6 +976,36 @@ __device__ __forceinline__ void adapt_tail(const GemmBArgs& g, Acc (&acc)[FM][FN
   }
 }
 
+// Layer*: the same for operands of either layout and every plane of A, rows in their own order.
+template <int FM, int FN, LayB LA, LayB LB, class Acc>
+__device__ __forceinline__ void layer_tail(const GemmBArgs& g, Acc (&acc)[FM][FN], int64_t mw, int64_t nw, int64_t k0,
+                                           int64_t k1, int lane) {
+  const int i = lane % 32, kg = 8 * (lane / 32);
+  auto frag = [](lr_u32x4 v) { return __builtin_bit_cast(bf16x8, v); };
+  for (int64_t k = k0; k < k1; k += 16) {
+    bf16x8 b[FN];
+#pragma unroll
+    for (int h = 0; h < FN; ++h) {
+      const int64_t n = min(nw + 32 * h + i, g.N - 1);
+      if constexpr (LB == LayB::KMajor) b[h] = frag(lr_load16(g.B + n * g.ldb + k + kg, k1 - k - kg));
+      else b[h] = frag(adapt_column(g.B, g.ldb, k, k1, n, kg));
+    }
+    for (int p = 0; p < g.ly.planes; ++p) {
+      const uint16_t* A = g.A + p * g.ly.plane_stride;
+#pragma unroll
+      for (int f = 0; f < FM; ++f) {
+        const int64_t m = min(mw + 32 * f + i, g.M - 1);
+        bf16x8 a;
+        if constexpr (LA == LayB::KMajor) a = frag(lr_load16(A + m * g.lda + k + kg, k1 - k - kg));
+        else a = frag(adapt_column(A, g.lda, k, k1, m, kg));
+#pragma unroll
+        for (int h = 0; h < FN; ++h) acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[h], acc[f][h], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);     // one fragment's operands in registers at a time
+      }
+    }
+  }
+}
+
 // Adapt*: the low-rank products of the tile's rows added to the sums (acc: 32 x 32 fragments of
 // wavefront rows wr.. and columns wc.. of the tile).  The block brings the 16-rank slices of all
 // adapters that its rows name into LDS (as many as fit into `bytes` at once: one
@@ -1037,7 +1153,8 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   const int64_t m0 = tm * BM, n0 = tn * BN;
   const int64_t kbeg = split * g.k_chunk;
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
-  const int nk = (int)((kend - kbeg) / BK);
+  const int nkp = (int)((kend - kbeg) / BK);             // whole k tiles, of each plane
+  const int nk = is_layer(EPI) ? nkp * g.ly.planes : nkp;
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
   if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at);
 
@@ -1046,11 +1163,21 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   else stage_offsets<LA, BM, BK, NW>(a_off, wid, lane, m0, g.M, g.lda);
   stage_offsets<LB, BN, BK, NW>(b_off, wid, lane, n0, g.N, g.ldb);
   // k tile kt into stage st
+  // (Layer*: consecutive calls take consecutive tiles, one plane after the other)
+  int64_t next_k = kbeg;
+  const uint16_t* next_a = g.A;
   auto issue = [&](int kt, int st) {
-    const int64_t k0 = kbeg + (int64_t)kt * BK;
+    const int64_t k0 = is_layer(EPI) ? next_k : kbeg + (int64_t)kt * BK;
     unsigned char* sa = smem + st * STAGE_BYTES;
-    stage_load<LA, NW>(g.A, a_off, k0, g.lda, sa, wid);
+    stage_load<LA, NW>(is_layer(EPI) ? next_a : g.A, a_off, k0, g.lda, sa, wid);
     stage_load<LB, NW>(g.B, b_off, k0, g.ldb, sa + A_CH * 16, wid);
+    if constexpr (is_layer(EPI)) {
+      next_k += BK;
+      if (next_k + BK > kend) {
+        next_k = kbeg;
+        next_a += g.ly.plane_stride;
+      }
+    }
   };
   typedef float f32x16 __attribute__((ext_vector_type(16)));
   auto frag_wait = [](bf16x8 (&af)[FM], bf16x8 (&bf)[FN]) {
@@ -1095,10 +1222,10 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   // receives tile t + S.
   for (int s = 0; s < S - 1; ++s)
     if (s < nk) issue(s, s);
-  // Small wave tiles (Adapt*) have too few MFMAs in a 16-deep step to cover its LDS reads: they read all
+  // Small wave tiles (Adapt*, Layer*) have too few MFMAs in a 16-deep step to cover its LDS reads: they read all
   // fragments of the next k tile while the current one is multiplied, with one wait and one
   // barrier per tile (1024 x 2048 x 2048 with 32 adapters on 64 x 64 tiles, k tile 64: 22 us, 25 by steps).
-  if constexpr (is_adapt(EPI)) {
+  if constexpr (is_adapt(EPI) || is_layer(EPI)) {
     typedef RawFrag<LA == LayB::KMajor> FragA;
     typedef RawFrag<LB == LayB::KMajor> FragB;
     FragA a0[KK][FM], a1[KK][FM];
@@ -1195,6 +1322,8 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   static_assert(S <= 4, "wait depth");
 
   bool odd = false;
+  if constexpr (is_layer(EPI))
+    layer_tail<FM, FN, LA, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nkp * BK, kend, lane);
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
     if (split == 0)
@@ -1286,7 +1415,8 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   const int64_t m0 = tm * BM, n0 = tn * BN;
   const int64_t kbeg = split * g.k_chunk;
   const int64_t kend = (kbeg + g.k_chunk < g.K) ? kbeg + g.k_chunk : g.K;
-  const int nk = (int)((kend - kbeg) / BK);
+  const int nkp = (int)((kend - kbeg) / BK);             // whole k tiles, of each plane
+  const int nk = is_layer(EPI) ? nkp * g.ly.planes : nkp;
   if constexpr (EPI == EpiB::MseBf) load_target_rows<BM>(g, m0, s_trow);
   if constexpr (is_adapt(EPI)) load_adapt_rows<BM>(g, m0, s_trow, s_at);
 
@@ -1294,11 +1424,21 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   if constexpr (is_adapt(EPI)) adapt_offsets<BM, BK, NW>(a_off, wid, lane, m0, g);
   else stage_offsets<LA, BM, BK, NW>(a_off, wid, lane, m0, g.M, g.lda);
   stage_offsets<LB, BN, BK, NW>(b_off, wid, lane, n0, g.N, g.ldb);
+  // (Layer*: consecutive calls take consecutive tiles, one plane after the other)
+  int64_t next_k = kbeg;
+  const uint16_t* next_a = g.A;
   auto issue = [&](int kt) {
-    const int64_t k0 = kbeg + (int64_t)kt * BK;
+    const int64_t k0 = is_layer(EPI) ? next_k : kbeg + (int64_t)kt * BK;
     unsigned char* sa = smem + (kt % S) * STAGE_BYTES;
-    stage_load<LA, NW>(g.A, a_off, k0, g.lda, sa, wid);
+    stage_load<LA, NW>(is_layer(EPI) ? next_a : g.A, a_off, k0, g.lda, sa, wid);
     stage_load<LB, NW>(g.B, b_off, k0, g.ldb, sa + A_CH * 16, wid);
+    if constexpr (is_layer(EPI)) {
+      next_k += BK;
+      if (next_k + BK > kend) {
+        next_k = kbeg;
+        next_a += g.ly.plane_stride;
+      }
+    }
   };
   typedef float f32x16 __attribute__((ext_vector_type(16)));
   constexpr int KK = BK / 16;
@@ -1380,6 +1520,8 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   }
 #undef OT_WAIT_VM
   bool odd = false;
+  if constexpr (is_layer(EPI))
+    layer_tail<FM, FN, LA, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nkp * BK, kend, lane);
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
     if (split == 0)

@@ -26,6 +26,7 @@
 
 #include "adam.h"
 #include "common.h"
+#include "layer_ops.h"
 #include "lowrank_ops.h"
 
 namespace ot {
@@ -43,9 +44,13 @@ enum class Epi : int {
   // gains the rows' low-rank product (split 0)
   AdaptF32 = 7,  // C (fp32) row perm[m] = acc (+ bias[n]) (ReLU, or 0 where lr.mask is not above 0)
   AdaptBf = 8,   // C (bf16) row perm[m] = the same, rounded
-  AdaptSplit = 9 // C[split] row m = acc
+  AdaptSplit = 9, // C[split] row m = acc
+  // Dense layers (dense.hip; gemm_f32x3_kernel only)
+  LayerF32 = 10, // C (fp32) = act(acc (+ bias[n])) (+ ly.residual, fp32); ly.pre (fp32) = acc (+ bias[n])
+  LayerBf = 11   // C (bf16) = bf16 of the same (residual bf16)
 };
 constexpr bool is_adapt(Epi e) { return e == Epi::AdaptF32 || e == Epi::AdaptBf || e == Epi::AdaptSplit; }
+constexpr bool is_layer(Epi e) { return e == Epi::LayerF32 || e == Epi::LayerBf; }
 
 struct GemmArgs {
   const float* A;
@@ -78,6 +83,7 @@ struct GemmArgs {
   float* bias_v;
   AdamArgs adam;
   AdaptRows lr;             // Adapt*
+  LayerArgs ly;             // Layer*
 };
 
 // Row sum of row m (the bias gradient) to where it goes; Adam on the bias element.

@@ -705,6 +705,58 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
     }
     return;
   }
+  if constexpr (is_layer(EPI)) {
+    constexpr bool BF = EPI == Epi::LayerBf;
+#pragma unroll
+    for (int h = 0; h < FN; ++h) bias[h] = g.bias && col_of(h) < g.N ? g.bias[col_of(h)] : 0.f;
+    // residuals of four rows are read together, before the lane writes the same columns of C, which may be the
+    // residual itself
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+      for (int r0 = 0; r0 < 16; r0 += 4) {
+        float res[4][FN];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int64_t m = min(row_of(f, r0 + u), g.M - 1);
+#pragma unroll
+          for (int h = 0; h < FN; ++h) res[u][h] = 0.f;
+          if (!g.ly.residual) continue;
+          if constexpr (BF) {
+            const uint16_t* p = static_cast<const uint16_t*>(g.ly.residual) + m * g.ly.ldr;
+#pragma unroll
+            for (int h = 0; h < FN; ++h)
+              if (col_of(h) < g.N) res[u][h] = lr_value(p + col_of(h));
+          } else {
+            get(static_cast<const float*>(g.ly.residual) + m * g.ly.ldr, res[u]);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int64_t m = row_of(f, r0 + u);
+          if (m >= g.M) continue;
+          float val[FN];
+#pragma unroll
+          for (int h = 0; h < FN; ++h) val[h] = acc[f][h][r0 + u] + bias[h];
+          if (g.ly.pre) put(static_cast<float*>(g.ly.pre) + m * g.ly.ldp, val);
+#pragma unroll
+          for (int h = 0; h < FN; ++h) val[h] = act_value(val[h], g.ly.act) + res[u][h];
+          if constexpr (BF) {
+            uint16_t* C = reinterpret_cast<uint16_t*>(g.C) + m * g.ldc;
+            if (IL && full) {
+              *reinterpret_cast<uint32_t*>(C + nw) = (uint32_t)lr_bf16(val[0]) | ((uint32_t)lr_bf16(val[FN - 1]) << 16);
+            } else {
+#pragma unroll
+              for (int h = 0; h < FN; ++h)
+                if (col_of(h) < g.N) C[col_of(h)] = lr_bf16(val[h]);
+            }
+          } else {
+            put(Cb + m * g.ldc, val);
+          }
+        }
+      }
+    return;
+  }
   float lsum = 0.f;
 #pragma unroll
   for (int f = 0; f < FM; ++f) {

@@ -1,0 +1,806 @@
+// Group norm with an activation over channels-last data (include/layers.h).
+//
+// Two forms.  Where a sample's group fits into LDS (8192 values), a block keeps some of a
+// sample's groups there: mean, then the squares of the differences from it, then the results, and
+// x is read once.  Longer groups take three launches: partial moments per chunk of
+// positions and channel, their join per sample and group, the results (x is read twice,
+// the second time from the Infinity Cache where it fits).  No atomics: every sum has a fixed order.
+#include <cmath>
+#include <new>
+
+#include "layer_host.h"
+#include "layer_ops.h"
+#include "layers.h"
+#include "norm_plan.h"
+#include "row_ops.h"
+#include "surrogate.h"
+
+namespace ot {
+
+struct NormArgs {
+  const void* x;
+  int64_t ldx;
+  const void* dy;           // backward
+  int64_t lddy;
+  void* out;                // y or dx (backward: nullable)
+  int64_t ldo;
+  const float* weight;      // nullable
+  const float* bias;        // nullable
+  const float* stats;       // backward: mean and rstd per sample and group
+  float* stats_out;         // forward (nullable)
+  int64_t n, positions, channels;
+  int32_t groups, per, act;
+  float eps;
+};
+
+// Sum over a team of S threads (S a power of two up to 256, teams aligned in the block), the same value to all; s:
+// four values per block, for teams of several wavefronts.  All threads of the block call it together.
+__device__ __forceinline__ float team_sum(float v, int S, float* s) {
+  for (int o = 1; o < S && o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+  if (S > 64) {                                          // the same for the whole block
+    const int wid = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) s[wid] = v;
+    __syncthreads();
+    if (S == 256) v = (s[0] + s[1]) + (s[2] + s[3]);
+    else v = s[wid & 2] + s[(wid & 2) + 1];
+    __syncthreads();
+  }
+  return v;
+}
+
+// What a block over slabs does with its groups: teams of S threads take one group after the
+// other; in a team CL threads lie side by side along the channels.
+struct Teams {
+  int S, CL, teams;
+  __device__ __forceinline__ Teams(int groups, int per) {
+    S = 256;
+    while (S > 1 && 256 / S < groups) S >>= 1;
+    CL = 1;
+    while (CL < S && CL < per) CL <<= 1;
+    teams = 256 / S;
+  }
+};
+
+// f(element index in the slab, channel in the block) over the values of group gi.
+template <class F>
+__device__ __forceinline__ void team_each(const Teams& t, int gi, int per, int positions, int width, F f) {
+  const int me = threadIdx.x % t.S, c0 = me % t.CL, p0 = me / t.CL, dp = t.S / t.CL;
+  for (int p = p0; p < positions; p += dp)
+    for (int c = c0; c < per; c += t.CL) f(p * width + gi * per + c, gi * per + c);
+}
+
+// A block's slab: sample s, groups g0 .., `width` channels from c0 on.  f(row, vector's channel in the block, values
+// of it that exist) over its vectors of 8 channels.
+template <class F>
+__device__ __forceinline__ void slab_each(int width, int positions, F f) {
+  const int vecs = (width + 7) / 8;
+  for (int i = threadIdx.x; i < vecs * positions; i += 256) {
+    const int p = i / vecs, c = i % vecs * 8;
+    f(p, c, width - c);
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void slab_load(const T* p, bool aligned, int left, float (&v)[8]) {
+  if (aligned) {
+    load8(p, left, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? lr_value(p + e) : 0.f;
+  }
+}
+template <class T>
+__device__ __forceinline__ void slab_store(T* p, bool aligned, int left, const float (&v)[8]) {
+  if (aligned) {
+    store8(p, left, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) lr_store(p + e, v[e]);
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void norm_slab_kernel(NormArgs a, int gb, int64_t parts) {
+  __shared__ float tile[kSlab];
+  __shared__ float s_mean[kSlabGroups], s_rstd[kSlabGroups], s_red[4];
+  const int P = (int)a.positions;
+  for (int64_t b = blockIdx.x; b < a.n * parts; b += gridDim.x) {
+    const int64_t s = b / parts, g0 = b % parts * gb;
+    const int groups = (int)min((int64_t)gb, a.groups - g0), width = groups * a.per;
+    const int64_t c0 = g0 * a.per;
+    const bool aligned = c0 % 8 == 0;
+    const T* x = static_cast<const T*>(a.x) + s * P * a.ldx + c0;
+    slab_each(width, P, [&](int p, int c, int left) {
+      float v[8];
+      slab_load(x + p * a.ldx + c, aligned, left, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < left) tile[p * width + c + e] = v[e];
+    });
+    __syncthreads();
+    const Teams t(groups, a.per);
+    const float inv = 1.f / (float)(a.per * P);
+    for (int i = 0; i < groups; i += t.teams) {            // every team takes part in every turn
+      const int gi = i + threadIdx.x / t.S;
+      const bool in = gi < groups;
+      float sum = 0.f;
+      if (in) team_each(t, gi, a.per, P, width, [&](int k, int) { sum += tile[k]; });
+      float mean = team_sum(sum, t.S, s_red) * inv;
+      // what the rounded sum left: the mean of the differences
+      sum = 0.f;
+      if (in) team_each(t, gi, a.per, P, width, [&](int k, int) { sum += tile[k] - mean; });
+      mean += team_sum(sum, t.S, s_red) * inv;
+      sum = 0.f;
+      if (in)
+        team_each(t, gi, a.per, P, width, [&](int k, int) {
+          const float d = tile[k] - mean;
+          sum = fmaf(d, d, sum);
+        });
+      const float var = team_sum(sum, t.S, s_red) * inv;
+      if (in && threadIdx.x % t.S == 0) {
+        const float rstd = 1.f / sqrtf(var + a.eps);
+        s_mean[gi] = mean;
+        s_rstd[gi] = rstd;
+        if (a.stats_out) {
+          float* o = a.stats_out + (s * a.groups + g0 + gi) * 2;
+          o[0] = mean;
+          o[1] = rstd;
+        }
+      }
+    }
+    __syncthreads();
+    T* y = static_cast<T*>(a.out) + s * P * a.ldo + c0;
+    slab_each(width, P, [&](int p, int c, int left) {
+      float v[8];
+      int gi = c / a.per, end = (gi + 1) * a.per;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = 0.f;
+        if (e < left) {
+          if (c + e >= end) {
+            ++gi;
+            end += a.per;
+          }
+          const float xh = (tile[p * width + c + e] - s_mean[gi]) * s_rstd[gi];
+          const int64_t ch = c0 + c + e;
+          v[e] = act_value(fmaf(xh, a.weight ? a.weight[ch] : 1.f, a.bias ? a.bias[ch] : 0.f), a.act);
+        }
+      }
+      slab_store(y + p * a.ldo + c, aligned, left, v);
+    });
+    __syncthreads();
+  }
+}
+
+// Block (range r of `ranges`, part of the groups): its samples one after the other; sums[0 / 1][range][channel]
+// receive the range's sums of dp xh and dp (nullable).
+template <class T>
+__global__ __launch_bounds__(256) void norm_slab_back_kernel(NormArgs a, int gb, int64_t parts, int64_t ranges,
+                                                             float* sums) {
+  __shared__ float t_dp[kSlab], t_xh[kSlab];
+  __shared__ float s_w[kSlab], s_b[kSlab];                 // sums of the range so far
+  __shared__ float s_c1[kSlabGroups], s_c2[kSlabGroups], s_red[4];
+  const int P = (int)a.positions;
+  const int64_t part = blockIdx.x % parts, range = blockIdx.x / parts;
+  const int64_t g0 = part * gb, c0 = g0 * a.per;
+  const int groups = (int)min((int64_t)gb, a.groups - g0), width = groups * a.per;
+  const bool aligned = c0 % 8 == 0;
+  const int64_t s0 = a.n * range / ranges, s1 = a.n * (range + 1) / ranges;
+  const Teams t(groups, a.per);
+  const float inv = 1.f / (float)(a.per * P);
+  for (int c = threadIdx.x; c < width; c += 256) s_w[c] = s_b[c] = 0.f;
+  for (int64_t s = s0; s < s1; ++s) {
+    const T* x = static_cast<const T*>(a.x) + s * P * a.ldx + c0;
+    const T* dy = static_cast<const T*>(a.dy) + s * P * a.lddy + c0;
+    const float* st = a.stats + (s * a.groups + g0) * 2;
+    __syncthreads();
+    slab_each(width, P, [&](int p, int c, int left) {
+      float v[8], d[8];
+      slab_load(x + p * a.ldx + c, aligned, left, v);
+      slab_load(dy + p * a.lddy + c, aligned, left, d);
+      int gi = c / a.per, end = (gi + 1) * a.per;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < left) {
+          if (c + e >= end) {
+            ++gi;
+            end += a.per;
+          }
+          const int64_t ch = c0 + c + e;
+          const float xh = (v[e] - st[2 * gi]) * st[2 * gi + 1];
+          t_xh[p * width + c + e] = xh;
+          t_dp[p * width + c + e] =
+              act_back(d[e], fmaf(xh, a.weight ? a.weight[ch] : 1.f, a.bias ? a.bias[ch] : 0.f), a.act);
+        }
+    });
+    __syncthreads();
+    if (sums)
+      for (int c = threadIdx.x; c < width; c += 256) {
+        float w = s_w[c], bsum = s_b[c];
+        for (int p = 0; p < P; ++p) {
+          const float d = t_dp[p * width + c];
+          w = fmaf(d, t_xh[p * width + c], w);
+          bsum += d;
+        }
+        s_w[c] = w;
+        s_b[c] = bsum;
+      }
+    if (!a.out) continue;
+    for (int i = 0; i < groups; i += t.teams) {
+      const int gi = i + threadIdx.x / t.S;
+      const bool in = gi < groups;
+      float c1 = 0.f, c2 = 0.f;
+      if (in)
+        team_each(t, gi, a.per, P, width, [&](int k, int c) {
+          const float d = t_dp[k] * (a.weight ? a.weight[c0 + c] : 1.f);
+          c1 += d;
+          c2 = fmaf(d, t_xh[k], c2);
+        });
+      c1 = team_sum(c1, t.S, s_red) * inv;
+      c2 = team_sum(c2, t.S, s_red) * inv;
+      if (in && threadIdx.x % t.S == 0) {
+        s_c1[gi] = c1;
+        s_c2[gi] = c2;
+      }
+    }
+    __syncthreads();
+    T* dx = static_cast<T*>(a.out) + s * P * a.ldo + c0;
+    slab_each(width, P, [&](int p, int c, int left) {
+      float v[8];
+      int gi = c / a.per, end = (gi + 1) * a.per;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = 0.f;
+        if (e < left) {
+          if (c + e >= end) {
+            ++gi;
+            end += a.per;
+          }
+          const int k = p * width + c + e;
+          const float d = t_dp[k] * (a.weight ? a.weight[c0 + c + e] : 1.f);
+          v[e] = st[2 * gi + 1] * ((d - s_c1[gi]) - t_xh[k] * s_c2[gi]);
+        }
+      }
+      slab_store(dx + p * a.ldo + c, aligned, left, v);
+    });
+  }
+  if (sums) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < width; c += 256) {
+      sums[range * a.channels + c0 + c] = s_w[c];
+      sums[(ranges + range) * a.channels + c0 + c] = s_b[c];
+    }
+  }
+}
+
+// Where block b of a split pass stands.
+struct NormSpot {
+  int64_t sample, chunk, r0, r1, c;      // rows r0 .. r1 of the data; this thread's first channel
+  int rx, lanes;                         // its row among those side by side
+  __device__ __forceinline__ NormSpot(const NormArgs& a, const NormPlan& p, int64_t b) {
+    const int64_t tile = b % p.tiles, q = b / p.tiles;
+    sample = q / p.chunks;
+    chunk = q % p.chunks;
+    lanes = 256 / p.col_threads;
+    rx = threadIdx.x / p.col_threads;
+    c = 8 * (tile * p.col_threads + threadIdx.x % p.col_threads);
+    r0 = sample * a.positions + chunk * p.rows;
+    r1 = sample * a.positions + min(a.positions, (chunk + 1) * p.rows);
+  }
+};
+
+// Mean and sum of squared differences of `na` and `nb` values (Chan, Golub, LeVeque: updating formulae for
+// sample variances).
+__device__ __forceinline__ void join_moments(float& mean, float& m2, float na, float mean_b, float m2_b, float nb) {
+  const float d = mean_b - mean, f = nb / (na + nb);
+  mean = fmaf(d, f, mean);
+  m2 = m2 + m2_b + d * d * (na * f);
+}
+
+// Moments of every channel of a chunk: [sample][chunk][channel] mean, then the sums of squares.  A thread's
+// rows are few, and it sums differences from the first of them, so that little cancels.
+template <class T>
+__global__ __launch_bounds__(256) void norm_moments_kernel(NormArgs a, NormPlan p, float* part) {
+  __shared__ float s_m[256][9], s_q[256][9];
+  const int64_t blocks = a.n * p.chunks * p.tiles;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const NormSpot at(a, p, b);
+    const int64_t left = a.channels - at.c;
+    float first[8], s1[8], s2[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) first[e] = s1[e] = s2[e] = 0.f;
+    int mine = 0;
+    if (left > 0) {
+      const T* x = static_cast<const T*>(a.x) + at.c;
+      int64_t r = at.r0 + at.rx;
+      if (r < at.r1) {
+        load8(x + r * a.ldx, left, first);
+        mine = 1;
+        r += at.lanes;
+      }
+#pragma unroll 4
+      for (; r < at.r1; r += at.lanes) {
+        float v[8];
+        load8(x + r * a.ldx, left, v);
+        ++mine;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float d = v[e] - first[e];
+          s1[e] += d;
+          s2[e] = fmaf(d, d, s2[e]);
+        }
+      }
+    }
+    const float inv = mine > 0 ? 1.f / (float)mine : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = s1[e] * inv;
+      s_m[threadIdx.x][e] = first[e] + m;
+      s_q[threadIdx.x][e] = fmaxf(0.f, fmaf(-s1[e], m, s2[e]));
+    }
+    // rows of lane rx: rx, rx + lanes, ..; joined pairwise
+    const int rows = (int)(at.r1 - at.r0);
+    auto count = [&](int rx, int step) { return rx < rows ? (rows - rx + step - 1) / step : 0; };
+    for (int h = at.lanes / 2; h > 0; h /= 2) {
+      __syncthreads();
+      if (at.rx < h) {
+        // after this turn lane rx holds the rows that are rx modulo h
+        const float na = (float)count(at.rx, 2 * h), nb = (float)count(at.rx + h, 2 * h);
+        if (nb > 0.f)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            join_moments(s_m[threadIdx.x][e], s_q[threadIdx.x][e], na, s_m[threadIdx.x + h * p.col_threads][e],
+                         s_q[threadIdx.x + h * p.col_threads][e], nb);
+      }
+    }
+    if (at.rx == 0) {
+      const int64_t o = (at.sample * p.chunks + at.chunk) * a.channels + at.c;
+      const int64_t q = a.n * p.chunks * a.channels;
+      for (int e = 0; e < 8; ++e)
+        if (e < left) {
+          part[o + e] = s_m[threadIdx.x][e];
+          part[q + o + e] = s_q[threadIdx.x][e];
+        }
+    }
+    __syncthreads();
+  }
+}
+
+// Block per sample and group: mean and rstd from the partial moments, in 64 bits.
+__global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a, NormPlan p, const float* part, float* stats) {
+  __shared__ double s_red[4];
+  const int64_t q = a.n * p.chunks * a.channels;
+  for (int64_t b = blockIdx.x; b < a.n * a.groups; b += gridDim.x) {
+    const int64_t s = b / a.groups, c0 = b % a.groups * a.per;
+    const int64_t values = p.chunks * a.per;
+    const float* mean_p = part + s * p.chunks * a.channels + c0;
+    auto rows = [&](int64_t chunk) { return (double)(min(a.positions, (chunk + 1) * p.rows) - chunk * p.rows); };
+    auto block_sum = [&](double v) {
+      v = warp_sum(v);
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = v;
+      __syncthreads();
+      return (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]);
+    };
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < values; i += 256) {
+      const int64_t k = i / a.per, c = i % a.per;
+      sum += rows(k) * (double)mean_p[k * a.channels + c];
+    }
+    const double total = (double)a.per * (double)a.positions;
+    const double mean = block_sum(sum) / total;
+    sum = 0.0;
+    for (int64_t i = threadIdx.x; i < values; i += 256) {
+      const int64_t k = i / a.per, c = i % a.per;
+      const double d = (double)mean_p[k * a.channels + c] - mean;
+      sum += (double)mean_p[q + k * a.channels + c] + rows(k) * d * d;
+    }
+    const double var = block_sum(sum) / total;
+    if (threadIdx.x == 0) {
+      const float m = (float)mean, rstd = (float)(1.0 / sqrt(var + (double)a.eps));
+      stats[2 * b] = m;
+      stats[2 * b + 1] = rstd;
+      if (a.stats_out) {
+        a.stats_out[2 * b] = m;
+        a.stats_out[2 * b + 1] = rstd;
+      }
+    }
+  }
+}
+
+// What a thread of a split pass keeps of its 8 channels.
+struct Channels {
+  float mean[8], rstd[8], w[8], b[8];
+  __device__ __forceinline__ Channels(const NormArgs& a, const float* stats, int64_t sample, int64_t c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t ch = min(c + e, a.channels - 1);
+      const float* s = stats + (sample * a.groups + ch / a.per) * 2;
+      mean[e] = s[0];
+      rstd[e] = s[1];
+      w[e] = a.weight ? a.weight[ch] : 1.f;
+      b[e] = a.bias ? a.bias[ch] : 0.f;
+    }
+  }
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void norm_apply_kernel(NormArgs a, NormPlan p, const float* stats) {
+  const int64_t blocks = a.n * p.chunks * p.tiles;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const NormSpot at(a, p, b);
+    const int64_t left = a.channels - at.c;
+    if (left <= 0) continue;
+    const Channels k(a, stats, at.sample, at.c);
+    const T* x = static_cast<const T*>(a.x) + at.c;
+    T* y = static_cast<T*>(a.out) + at.c;
+#pragma unroll 2
+    for (int64_t r = at.r0 + at.rx; r < at.r1; r += at.lanes) {
+      float v[8];
+      load8(x + r * a.ldx, left, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = act_value(fmaf((v[e] - k.mean[e]) * k.rstd[e], k.w[e], k.b[e]), a.act);
+      store8(y + r * a.ldo, left, v);
+    }
+  }
+}
+
+// Sums of dp xh and dp over a chunk's rows: [sample][chunk][channel] of each.
+template <class T>
+__global__ __launch_bounds__(256) void norm_sums_kernel(NormArgs a, NormPlan p, float* part) {
+  __shared__ float s_w[256][9], s_b[256][9];
+  const int64_t blocks = a.n * p.chunks * p.tiles;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const NormSpot at(a, p, b);
+    const int64_t left = a.channels - at.c;
+    float sw[8], sb[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sw[e] = sb[e] = 0.f;
+    if (left > 0) {
+      const Channels k(a, a.stats, at.sample, at.c);
+      const T* x = static_cast<const T*>(a.x) + at.c;
+      const T* dy = static_cast<const T*>(a.dy) + at.c;
+#pragma unroll 2
+      for (int64_t r = at.r0 + at.rx; r < at.r1; r += at.lanes) {
+        float v[8], d[8];
+        load8(x + r * a.ldx, left, v);
+        load8(dy + r * a.lddy, left, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float xh = (v[e] - k.mean[e]) * k.rstd[e];
+          const float dp = act_back(d[e], fmaf(xh, k.w[e], k.b[e]), a.act);
+          sw[e] = fmaf(dp, xh, sw[e]);
+          sb[e] += dp;
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s_w[threadIdx.x][e] = sw[e];
+      s_b[threadIdx.x][e] = sb[e];
+    }
+    for (int h = at.lanes / 2; h > 0; h /= 2) {
+      __syncthreads();
+      if (at.rx < h)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s_w[threadIdx.x][e] += s_w[threadIdx.x + h * p.col_threads][e];
+          s_b[threadIdx.x][e] += s_b[threadIdx.x + h * p.col_threads][e];
+        }
+    }
+    if (at.rx == 0) {
+      const int64_t o = (at.sample * p.chunks + at.chunk) * a.channels + at.c;
+      const int64_t q = a.n * p.chunks * a.channels;
+      for (int e = 0; e < 8; ++e)
+        if (e < left) {
+          part[o + e] = s_w[threadIdx.x][e];
+          part[q + o + e] = s_b[threadIdx.x][e];
+        }
+    }
+    __syncthreads();
+  }
+}
+
+// Block per sample and group: the means of weight dp and weight dp xh (coef), and the sample's sums per
+// channel (sums[0 / 1][sample][channel]).
+__global__ __launch_bounds__(256) void norm_coef_kernel(NormArgs a, NormPlan p, const float* part, float* coef,
+                                                        float* sums) {
+  __shared__ double s_red[2][4];
+  const int64_t q = a.n * p.chunks * a.channels;
+  for (int64_t b = blockIdx.x; b < a.n * a.groups; b += gridDim.x) {
+    const int64_t s = b / a.groups, c0 = b % a.groups * a.per;
+    const float* pw = part + s * p.chunks * a.channels + c0;
+    double c1 = 0.0, c2 = 0.0;
+    for (int64_t c = threadIdx.x; c < a.per; c += 256) {
+      double w = 0.0, d = 0.0;
+      for (int64_t k = 0; k < p.chunks; ++k) {
+        w += (double)pw[k * a.channels + c];
+        d += (double)pw[q + k * a.channels + c];
+      }
+      sums[s * a.channels + c0 + c] = (float)w;
+      sums[(a.n + s) * a.channels + c0 + c] = (float)d;
+      const double g = a.weight ? (double)a.weight[c0 + c] : 1.0;
+      c1 += g * d;
+      c2 += g * w;
+    }
+    c1 = warp_sum(c1);
+    c2 = warp_sum(c2);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+      s_red[0][threadIdx.x >> 6] = c1;
+      s_red[1][threadIdx.x >> 6] = c2;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+      const double* r = s_red[threadIdx.x];
+      coef[2 * b + threadIdx.x] =
+          (float)(((r[0] + r[1]) + (r[2] + r[3])) / ((double)a.per * (double)a.positions));
+    }
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void norm_apply_back_kernel(NormArgs a, NormPlan p, const float* coef) {
+  const int64_t blocks = a.n * p.chunks * p.tiles;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const NormSpot at(a, p, b);
+    const int64_t left = a.channels - at.c;
+    if (left <= 0) continue;
+    const Channels k(a, a.stats, at.sample, at.c);
+    float c1[8], c2[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float* s = coef + (at.sample * a.groups + min(at.c + e, a.channels - 1) / a.per) * 2;
+      c1[e] = s[0];
+      c2[e] = s[1];
+    }
+    const T* x = static_cast<const T*>(a.x) + at.c;
+    const T* dy = static_cast<const T*>(a.dy) + at.c;
+    T* dx = static_cast<T*>(a.out) + at.c;
+#pragma unroll 2
+    for (int64_t r = at.r0 + at.rx; r < at.r1; r += at.lanes) {
+      float v[8], d[8];
+      load8(x + r * a.ldx, left, v);
+      load8(dy + r * a.lddy, left, d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float xh = (v[e] - k.mean[e]) * k.rstd[e];
+        const float dp = act_back(d[e], fmaf(xh, k.w[e], k.b[e]), a.act) * k.w[e];
+        v[e] = k.rstd[e] * ((dp - c1[e]) - xh * c2[e]);
+      }
+      store8(dx + r * a.ldo, left, v);
+    }
+  }
+}
+
+// out[c] = sum over k of part[k][c] in a fixed order, for both gradients (blockIdx.y): a block takes 64
+// channels, its 16 wavefronts each a sixteenth of the rows.
+__global__ __launch_bounds__(1024) void norm_gradient_kernel(const float* __restrict__ part, int64_t rows,
+                                                             int64_t channels, float* dweight, float* dbias) {
+  __shared__ float s[16][64];
+  float* out = blockIdx.y ? dbias : dweight;
+  if (!out) return;                                      // the same for the whole block
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  const float* p = part + blockIdx.y * rows * channels;
+  float sum = 0.f;
+  if (c < channels)
+#pragma unroll 8
+    for (int64_t k = wid; k < rows; k += 16) sum += p[k * channels + c];
+  s[wid][lane] = sum;
+  __syncthreads();
+  if (wid == 0 && c < channels) {
+    for (int k = 1; k < 16; ++k) sum += s[k][lane];
+    out[c] = sum;
+  }
+}
+
+}  // namespace ot
+
+struct ot_norm {
+  ot::NormSizes sizes;
+  int32_t precision, act;
+  float eps;
+  int device;
+  ot::Workspace ws;
+  int64_t bytes(int64_t n) const { return 4 * ot::norm_values(sizes, n); }
+};
+
+namespace {
+
+constexpr int64_t kMostSamples = 1LL << 26, kMostValues = 1LL << 36;
+constexpr int64_t kMostBlocks = 1LL << 20;              // kernels loop over what is more
+
+unsigned grid_of(int64_t blocks) { return (unsigned)std::min(blocks, kMostBlocks); }
+
+ot::NormArgs args_of(const ot_norm* d, int64_t n) {
+  ot::NormArgs a{};
+  a.n = n;
+  a.positions = d->sizes.positions;
+  a.channels = d->sizes.channels;
+  a.groups = d->sizes.groups;
+  a.per = (int32_t)d->sizes.per();
+  a.act = d->act;
+  a.eps = d->eps;
+  return a;
+}
+
+template <class T>
+int forward(const ot_norm* d, const ot::NormArgs& a, hipStream_t st) {
+  const int gb = ot::slab_groups(d->sizes);
+  if (gb > 0) {
+    const int64_t parts = ot::ceil_div(a.groups, gb);
+    hipLaunchKernelGGL(ot::norm_slab_kernel<T>, dim3(grid_of(a.n * parts)), dim3(256), 0, st, a, gb, parts);
+    OT_LAUNCHED("norm_slab_kernel");
+    return OT_OK;
+  }
+  const ot::NormPlan p = ot::plan_norm(d->sizes, a.n);
+  float* stats = reinterpret_cast<float*>(d->ws.p);
+  float* part = stats + 2 * a.n * a.groups;
+  const dim3 grid(grid_of(a.n * p.chunks * p.tiles));
+  hipLaunchKernelGGL(ot::norm_moments_kernel<T>, grid, dim3(256), 0, st, a, p, part);
+  OT_LAUNCHED("norm_moments_kernel");
+  hipLaunchKernelGGL(ot::norm_join_kernel, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, stats);
+  OT_LAUNCHED("norm_join_kernel");
+  hipLaunchKernelGGL(ot::norm_apply_kernel<T>, grid, dim3(256), 0, st, a, p, stats);
+  OT_LAUNCHED("norm_apply_kernel");
+  return OT_OK;
+}
+
+int gradients(const float* sums, int64_t rows, int64_t channels, float* dweight, float* dbias, hipStream_t st) {
+  hipLaunchKernelGGL(ot::norm_gradient_kernel, dim3((unsigned)ot::ceil_div(channels, 64), 2), dim3(1024), 0, st, sums,
+                     rows, channels, dweight, dbias);
+  OT_LAUNCHED("norm_gradient_kernel");
+  return OT_OK;
+}
+
+template <class T>
+int backward(const ot_norm* d, const ot::NormArgs& a, float* dweight, float* dbias, hipStream_t st) {
+  const int gb = ot::slab_groups(d->sizes);
+  const bool want = dweight || dbias;
+  float* ws = reinterpret_cast<float*>(d->ws.p);
+  if (gb > 0) {
+    const int64_t parts = ot::ceil_div(a.groups, gb), ranges = ot::slab_ranges(d->sizes, a.n);
+    hipLaunchKernelGGL(ot::norm_slab_back_kernel<T>, dim3((unsigned)(parts * ranges)), dim3(256), 0, st, a, gb, parts,
+                       ranges, want ? ws : nullptr);
+    OT_LAUNCHED("norm_slab_back_kernel");
+    return want ? gradients(ws, ranges, a.channels, dweight, dbias, st) : OT_OK;
+  }
+  const ot::NormPlan p = ot::plan_norm(d->sizes, a.n);
+  float* coef = ws;
+  float* sums = coef + 2 * a.n * a.groups;
+  float* part = sums + 2 * a.n * a.channels;
+  const dim3 grid(grid_of(a.n * p.chunks * p.tiles));
+  hipLaunchKernelGGL(ot::norm_sums_kernel<T>, grid, dim3(256), 0, st, a, p, part);
+  OT_LAUNCHED("norm_sums_kernel");
+  hipLaunchKernelGGL(ot::norm_coef_kernel, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, coef, sums);
+  OT_LAUNCHED("norm_coef_kernel");
+  if (a.out) {
+    hipLaunchKernelGGL(ot::norm_apply_back_kernel<T>, grid, dim3(256), 0, st, a, p, coef);
+    OT_LAUNCHED("norm_apply_back_kernel");
+  }
+  return want ? gradients(sums, a.n, a.channels, dweight, dbias, st) : OT_OK;
+}
+
+}  // namespace
+
+extern "C" int norm_create(ot_norm** out, int64_t channels, int32_t groups, int64_t positions, int32_t precision,
+                           int32_t activation, float eps, int64_t max_samples) {
+  ot::clear_error();
+  OT_REQUIRE(out != nullptr, "norm_create: NULL out");
+  *out = nullptr;
+  OT_REQUIRE(channels >= 1 && channels <= 65536, "norm_create: channels outside [1, 65536]");
+  OT_REQUIRE(groups >= 1 && groups <= channels && channels % groups == 0, "norm_create: groups do not divide channels");
+  OT_REQUIRE(positions >= 1 && positions <= (1LL << 26), "norm_create: positions outside [1, 2^26]");
+  OT_REQUIRE(precision == OT_FP32 || precision == OT_BF16, "norm_create: unknown precision");
+  OT_REQUIRE(activation >= OT_ACT_NONE && activation <= OT_ACT_GELU, "norm_create: unknown activation");
+  OT_REQUIRE(std::isfinite(eps) && eps > 0.f, "norm_create: eps is not finite and above 0");
+  OT_REQUIRE(max_samples >= 0 && max_samples <= kMostSamples, "norm_create: max_samples outside [0, 2^26]");
+  OT_REQUIRE(channels * positions <= kMostValues && max_samples <= kMostValues / (channels * positions),
+             "norm_create: more than 2^36 values");
+  int device = -1;
+  OT_HIP(hipGetDevice(&device));
+  ot_norm* d = new (std::nothrow) ot_norm();
+  if (!d) return ot::set_error(OT_E_NOMEM, "norm_create: out of host memory");
+  d->sizes = ot::NormSizes{channels, positions, groups};
+  d->precision = precision;
+  d->act = activation;
+  d->eps = eps;
+  d->device = device;
+  const int rc = d->ws.allocate(max_samples, d->bytes(max_samples), "norm_create");
+  if (rc) {
+    delete d;
+    return rc;
+  }
+  *out = d;
+  return OT_OK;
+}
+
+namespace {
+
+// Checks that forward and backward share.
+int check_call(const ot_norm* d, const void* x, int64_t ldx, const float* weight, const float* bias, int64_t n,
+               const char* what) {
+  OT_REQUIRE(n >= 0 && n <= kMostSamples, "%s: n outside [0, 2^26]", what);
+  OT_REQUIRE(n <= kMostValues / (d->sizes.channels * d->sizes.positions), "%s: more than 2^36 values", what);
+  if (n == 0) return OT_OK;
+  const int e = d->precision == OT_BF16 ? 2 : 4;
+  int rc;
+  if ((rc = ot::check_rows(x, ldx, n * d->sizes.positions, d->sizes.channels, e, what, "x"))) return rc;
+  if ((rc = ot::check_values(weight, 4, what, "weight"))) return rc;
+  return ot::check_values(bias, 4, what, "bias");
+}
+
+}  // namespace
+
+extern "C" int norm_forward(ot_norm* d, const void* x, int64_t ldx, const float* weight, const float* bias, int64_t n,
+                            void* y, int64_t ldy, float* stats, void* stream) try {
+  ot::clear_error();
+  const char* what = "norm_forward";
+  OT_REQUIRE(d != nullptr, "%s: NULL norm", what);
+  int rc;
+  if ((rc = check_call(d, x, ldx, weight, bias, n, what)) || n == 0) return rc;
+  const int e = d->precision == OT_BF16 ? 2 : 4;
+  if ((rc = ot::check_rows(y, ldy, n * d->sizes.positions, d->sizes.channels, e, what, "y"))) return rc;
+  if ((rc = ot::check_values(stats, 4, what, "stats"))) return rc;
+  if ((rc = ot::check_device(d->device, what))) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if ((rc = d->ws.begin(n, st, what, [&](int64_t k) { return d->bytes(k); }))) return rc;
+  ot::NormArgs a = args_of(d, n);
+  a.x = x;
+  a.ldx = ldx;
+  a.out = y;
+  a.ldo = ldy;
+  a.weight = weight;
+  a.bias = bias;
+  a.stats_out = stats;
+  return e == 2 ? forward<uint16_t>(d, a, st) : forward<float>(d, a, st);
+} catch (const std::bad_alloc&) {
+  return ot::set_error(OT_E_NOMEM, "norm_forward: out of host memory");
+}
+
+extern "C" int norm_backward(ot_norm* d, const void* x, int64_t ldx, const float* weight, const float* bias,
+                             int64_t n, const float* stats, const void* dy, int64_t lddy, void* dx, int64_t lddx,
+                             float* dweight, float* dbias, void* stream) try {
+  ot::clear_error();
+  const char* what = "norm_backward";
+  OT_REQUIRE(d != nullptr, "%s: NULL norm", what);
+  int rc;
+  if ((rc = check_call(d, x, ldx, weight, bias, n, what))) return rc;
+  if ((rc = ot::check_values(dweight, 4, what, "dweight"))) return rc;
+  if ((rc = ot::check_values(dbias, 4, what, "dbias"))) return rc;
+  const int e = d->precision == OT_BF16 ? 2 : 4;
+  if (n > 0) {
+    OT_REQUIRE(stats != nullptr, "%s: NULL stats", what);
+    if ((rc = ot::check_values(stats, 4, what, "stats"))) return rc;
+    if ((rc = ot::check_rows(dy, lddy, n * d->sizes.positions, d->sizes.channels, e, what, "dy"))) return rc;
+    if (dx && (rc = ot::check_rows(dx, lddx, n * d->sizes.positions, d->sizes.channels, e, what, "dx"))) return rc;
+  }
+  if ((rc = ot::check_device(d->device, what))) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (n == 0) return dweight || dbias ? gradients(nullptr, 0, d->sizes.channels, dweight, dbias, st) : OT_OK;
+  if (!dx && !dweight && !dbias) return OT_OK;
+  if ((rc = d->ws.begin(n, st, what, [&](int64_t k) { return d->bytes(k); }))) return rc;
+  ot::NormArgs a = args_of(d, n);
+  a.x = x;
+  a.ldx = ldx;
+  a.dy = dy;
+  a.lddy = lddy;
+  a.out = dx;
+  a.ldo = lddx;
+  a.weight = weight;
+  a.bias = bias;
+  a.stats = stats;
+  return e == 2 ? backward<uint16_t>(d, a, dweight, dbias, st) : backward<float>(d, a, dweight, dbias, st);
+} catch (const std::bad_alloc&) {
+  return ot::set_error(OT_E_NOMEM, "norm_backward: out of host memory");
+}
+
+extern "C" int norm_destroy(ot_norm* d) {
+  ot::clear_error();
+  if (!d) return OT_OK;
+  d->ws.release();
+  delete d;
+  return OT_OK;
+}

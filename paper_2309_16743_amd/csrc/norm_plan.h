@@ -1,0 +1,74 @@
+// Launch shapes and workspaces of group norm (norm.hip), free of HIP, so that they can be checked on the
+// CPU.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+
+#include "intmath.h"
+
+namespace ot {
+
+struct NormSizes {
+  int64_t channels, positions;
+  int32_t groups;
+  int64_t per() const { return channels / groups; }     // channels of a group
+};
+
+// Groups of a sample whose values fit here are kept in LDS as fp32, so that they are read once.
+constexpr int64_t kSlab = 8192;
+constexpr int32_t kSlabGroups = 1024;
+
+// Groups of one block (0: a group does not fit, the passes are split): whole vectors of 8 channels where that
+// can be had.
+inline int32_t slab_groups(const NormSizes& s) {
+  const int64_t fit = std::min<int64_t>(std::min<int64_t>(s.groups, kSlabGroups), kSlab / (s.per() * s.positions));
+  if (fit >= s.groups || fit < 1) return (int32_t)fit;
+  for (int64_t g = fit; g >= 1; --g)
+    if (g * s.per() % 8 == 0) return (int32_t)g;
+  return (int32_t)fit;
+}
+
+// Split passes: a block holds col_threads x 8 channels (tiles of them cover the row) and a chunk of `rows`
+// positions of one sample.
+struct NormPlan {
+  int32_t col_threads;
+  int64_t tiles, chunks, rows;
+};
+constexpr int64_t kNormBlocks = 1024;
+inline NormPlan plan_norm(const NormSizes& s, int64_t n) {
+  NormPlan p{};
+  const int64_t vecs = ceil_div(s.channels, 8);
+  p.col_threads = 1;
+  while (p.col_threads < 256 && p.col_threads < vecs) p.col_threads *= 2;
+  p.tiles = ceil_div(vecs, p.col_threads);
+  const int64_t lanes = 256 / p.col_threads;
+  // 16 rows a thread, 64 a block at least; fewer while the card is not filled
+  int64_t chunks = ceil_div(s.positions, std::max<int64_t>(16 * lanes, 64));
+  if (n * p.tiles * chunks < kNormBlocks)
+    chunks = std::max(chunks, std::min(ceil_div(kNormBlocks, n * p.tiles), ceil_div(s.positions, 2 * lanes)));
+  p.rows = ceil_div(ceil_div(s.positions, chunks), lanes) * lanes;
+  p.chunks = ceil_div(s.positions, p.rows);
+  return p;
+}
+
+// Sample ranges that the backward over slabs keeps sums of.
+inline int64_t slab_ranges(const NormSizes& s, int64_t n) {
+  const int64_t parts = ceil_div(s.groups, slab_groups(s));
+  return std::max<int64_t>(1, std::min(n, kNormBlocks / parts));
+}
+
+// fp32 values that calls of up to n samples need: split passes keep two sums per channel and chunk, and
+// two values per sample and group; the backward also two sums per sample and channel.  Over slabs the
+// backward keeps two sums per range and channel.
+inline int64_t norm_values(const NormSizes& s, int64_t n) {
+  if (n < 1) return 0;
+  if (slab_groups(s) > 0) return 2 * s.channels * std::min(n, kNormBlocks);
+  const NormPlan most = plan_norm(s, n);
+  const int64_t lanes = 256 / most.col_threads;
+  const int64_t all = n * ceil_div(s.positions, std::max<int64_t>(16 * lanes, 64));
+  const int64_t chunks = std::max(all, std::min(ceil_div(kNormBlocks, most.tiles) + n, n * ceil_div(s.positions, 2 * lanes)));
+  return 2 * (chunks * s.channels + n * s.channels + n * s.groups);
+}
+
+}  // namespace ot

@@ -1,0 +1,236 @@
+"""The dense layer against the 64-bit reference (tolerances: layer_checks)."""
+import numpy as np
+import pytest
+import torch
+
+from layer_checks import DEV, U, close, half, host, like, padded, padding_kept, vector
+from layer_sizes import DENSE
+from oracle import layers as ref
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+ACTS = ["none", "relu", "silu", "gelu"]
+
+
+def layer(n_in, n_out, dtype, name="none", max_rows=4096):
+    import paper_2309_16743_amd as ot
+    return ot.DenseLayer(n_in, n_out, precision=ot.OT_BF16 if dtype == BF16 else ot.OT_FP32,
+                         activation=ACTS.index(name), max_rows=max_rows)
+
+
+def problem(n, n_in, n_out, dtype, seed, extra=0):
+    rng = np.random.default_rng(seed)
+    x = padded(rng.normal(size=(n, n_in)), dtype, extra)
+    w = padded(rng.normal(size=(n_out, n_in)) / np.sqrt(n_in), dtype, extra)
+    return rng, x, w, vector(rng.uniform(-0.5, 0.5, n_out))
+
+
+def forward_tol(x, w, b, r, y, y_type, k):
+    """Of z: the sum's; of y: the same through a slope of at most 1.13, the activation's own, the residual's sum."""
+    s = np.abs(x) @ np.abs(w).T + (0 if b is None else np.abs(b))
+    z = (4 * np.sqrt(k) + 8) * U * s
+    return z, 1.13 * z + 80 * U * (np.abs(y) + (0 if r is None else np.abs(r))) + half(y_type) * np.abs(y)
+
+
+@pytest.mark.parametrize("dtype,y_type", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("i", range(len(DENSE)))
+def test_forward(i, dtype, y_type):
+    n, n_in, n_out = DENSE[i]
+    name, extra = ACTS[i % 4], 8 * (i % 3)
+    rng, x, w, b = problem(n, n_in, n_out, dtype, 10 + i, extra)
+    b = b if i % 5 else None
+    r = padded(rng.normal(size=(n, n_out)), y_type, extra) if i % 2 else None
+    y = like((n, n_out), y_type, extra)
+    pre = like((n, n_out), dtype, extra) if i % 3 else None
+    op = layer(n_in, n_out, dtype, name, 0)
+    op.forward(x, w, y, bias=b, residual=r, pre=pre)
+    hx, hw = host(x), host(w)
+    hb, hr = None if b is None else host(b), None if r is None else host(r)
+    want, z = ref.dense(hx, hw, hb, hr, name)
+    tz, ty = forward_tol(hx, hw, hb, hr, want, y_type, n_in)
+    close(y, want, ty, "y")
+    padding_kept(y, 7.0)
+    if pre is not None:
+        close(pre, z, tz + half(dtype) * np.abs(z), "pre")
+        padding_kept(pre, 7.0)
+    op.close()
+
+
+def backward_tols(x, w, dy, pre, name, k_dx, k_dw):
+    """Sums over absolute values; dz is off by 40 u of dy and rounded by u."""
+    a = np.abs(dy) if pre is None or name == "relu" else 1.13 * np.abs(dy)
+    if name in ("silu", "gelu"):
+        extra = 45
+    else:
+        extra = 0
+    s_dx, s_dw, s_db = a @ np.abs(w), a.T @ np.abs(x), a.sum(0)
+    f = lambda k: (4 * np.sqrt(k) + 8 + extra) * U
+    return f(k_dx) * s_dx, f(k_dw) * s_dw, f(k_dw) * s_db
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("i", range(len(DENSE)))
+def test_backward(i, dtype):
+    n, n_in, n_out = DENSE[i]
+    name, extra = ACTS[(i + 1) % 4], 8 * (i % 3)
+    rng, x, w, _ = problem(n, n_in, n_out, dtype, 40 + i, extra)
+    dy = padded(rng.normal(size=(n, n_out)), dtype, extra)
+    pre = padded(rng.normal(size=(n, n_out)), dtype) if name != "none" else None
+    dx, dw, db = like((n, n_in), dtype, extra), like((n_out, n_in), F32, extra), vector(np.full(n_out, 7.0))
+    op = layer(n_in, n_out, dtype, name, n)
+    op.backward(x, w, dy, pre=pre, dx=dx, dw=dw, dbias=db)
+    hx, hw, hdy = host(x), host(w), host(dy)
+    hp = None if pre is None else host(pre)
+    want = ref.dense_back(hx, hw, hdy, hp, name)
+    tol = backward_tols(hx, hw, hdy, hp, name, n_out, n)
+    close(dx, want[0], tol[0] + half(dtype) * np.abs(want[0]), "dx")
+    close(dw, want[1], tol[1] + U * np.abs(want[1]), "dw")
+    close(db, want[2], tol[2] + U * np.abs(want[2]), "dbias")
+    padding_kept(dx, 7.0)
+    padding_kept(dw, 7.0)
+    # each gradient alone has the same bits
+    for kind in ("dx", "dw", "dbias"):
+        one = {"dx": like((n, n_in), dtype), "dw": like((n_out, n_in)), "dbias": vector(np.zeros(n_out))}[kind]
+        op.backward(x if kind == "dw" else None, w if kind == "dx" else None, dy, pre=pre, **{kind: one})
+        assert torch.equal(one, {"dx": dx, "dw": dw, "dbias": db}[kind]), kind
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_training_pair_with_one_product(dtype):
+    """forward's pre goes into backward: gradients of the whole function against the 64-bit ones and against
+    differences of the function the device computes."""
+    n, n_in, n_out, name = 12, 20, 9, "gelu"
+    rng, x, w, b = problem(n, n_in, n_out, F32, 3)
+    if dtype == BF16:
+        x, w = padded(host(x), BF16), padded(host(w), BF16)
+    dy = padded(rng.normal(size=(n, n_out)), dtype)
+    op = layer(n_in, n_out, dtype, name)
+    y, pre = like((n, n_out)), like((n, n_out), dtype)
+    op.forward(x, w, y, bias=b, pre=pre)
+    dw, db = like((n_out, n_in)), vector(np.zeros(n_out))
+    op.backward(x, w, dy, pre=pre, dw=dw, dbias=db)
+    hx, hw, hdy = host(x), host(w), host(dy)
+    z = ref.dense(hx, hw, host(b), None, name)[1]
+    # pre's rounding moves a slope by at most 0.8 (the largest second derivative of gelu) times half an eps of z
+    dw_ref, db_ref = ref.dense_back(hx, hw, hdy, z, name)[1:]
+    move = np.abs(hdy) * (0.8 * (half(dtype) + 40 * U) * np.abs(z) + 60 * U)
+    close(dw, dw_ref, move.T @ np.abs(hx) + 1e-6, "dw")
+    close(db, db_ref, move.sum(0) + 1e-6, "dbias")
+    if dtype == F32:
+        # a difference over 2 h: rounding of the outputs (1e-6 of values of size 1, summed with 108 weights of size
+        # 1) over 2 h, and a curvature below 2 h^2 times the same sum
+        h = 2.0 ** -6
+        for at in ((0, 0), (4, 11), (8, 19)):
+            vals = []
+            for sign in (1, -1):
+                moved = padded(hw)
+                moved[at] += sign * h
+                op.forward(x, moved, y, bias=b)
+                vals.append((host(y) * hdy).sum())
+            assert abs((vals[0] - vals[1]) / (2 * h) - host(dw)[at]) < 1e-6 * 108 / h + 2 * h * h * 108
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_rows(dtype):
+    op = layer(5, 9, dtype, "silu", 4)
+    x, w, y = like((0, 5), dtype), like((9, 5), dtype), like((0, 9), dtype)
+    op.forward(x, w, y)
+    dw, db = like((9, 5)), vector(np.full(9, 7.0))
+    op.backward(x, w, y, pre=y, dx=like((0, 5), dtype), dw=dw, dbias=db)
+    assert not host(dw).any() and not host(db).any()
+    padding_kept(dw, 7.0)
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [3, 40, 300])
+def test_the_residual_may_be_the_output(dtype, n):
+    rng, x, w, b = problem(n, 70, 133, dtype, 5)
+    h = padded(rng.normal(size=(n, 133)), dtype)
+    y = like((n, 133), dtype)
+    op = layer(70, 133, dtype, "gelu", 0)
+    op.forward(x, w, y, bias=b, residual=h)
+    op.forward(x, w, h, bias=b, residual=h)
+    assert torch.equal(y, h)
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_and_columns_keep_their_special_values(dtype):
+    """An infinity or NaN in a row of x, a row of W, the bias or the residual reaches what the formula says and nothing
+    else (finite parts keep to the tolerance); NaN passes relu."""
+    n, n_in, n_out = 70, 45, 200
+    for name in ("none", "relu"):
+        rng, x, w, b = problem(n, n_in, n_out, dtype, 6)
+        r = padded(rng.normal(size=(n, n_out)), dtype)
+        x[3, 44] = float("inf")
+        x[5, 0] = float("nan")
+        w[7, 2] = float("-inf")
+        b[11] = float("nan")
+        r[9, 13] = float("inf")
+        y = like((n, n_out), dtype)
+        op = layer(n_in, n_out, dtype, name, 0)
+        op.forward(x, w, y, bias=b, residual=r)
+        with np.errstate(invalid="ignore"):
+            want = ref.dense(host(x), host(w), host(b), host(r), name)[0]
+        got = host(y)
+        bad = ~np.isfinite(want)
+        assert bad.any() and not bad.all()
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.array_equal(got[bad & ~np.isnan(want)], want[bad & ~np.isnan(want)])
+        hx, hw = np.nan_to_num(host(x), posinf=0), np.nan_to_num(host(w), neginf=0)
+        tol = forward_tol(hx, hw, np.nan_to_num(host(b)), None, np.where(bad, 0, want), dtype, n_in)[1]
+        close(np.where(bad, 0, got), np.where(bad, 0, want), tol + 80 * U * np.abs(np.where(bad, 0, host(r))))
+        op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_relu_drops_infinite_gradients(dtype):
+    """dy that is not finite where relu is off reaches nothing."""
+    n, n_in, n_out = 40, 33, 50
+    rng, x, w, _ = problem(n, n_in, n_out, dtype, 7)
+    hd, hp = rng.normal(size=(n, n_out)), rng.normal(size=(n, n_out))
+    dy, pre = padded(hd, dtype), padded(hp, dtype)
+    clean = padded(np.where(hp > 0, hd, 0), dtype)
+    off = host(pre) <= 0
+    dy[torch.from_numpy(off).to(DEV)] = float("inf")
+    op = layer(n_in, n_out, dtype, "relu", n)
+    out = []
+    for g in (dy, clean):
+        dx, dw, db = like((n, n_in), dtype), like((n_out, n_in)), vector(np.zeros(n_out))
+        op.backward(x, w, g, pre=pre, dx=dx, dw=dw, dbias=db)
+        out.append((dx, dw, db))
+    for a, b in zip(*out):
+        assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_row_offsets_past_32_bits(dtype):
+    """Rows of x, W and y that lie 2^29 values apart (slices of one wide array)."""
+    e = 2 if dtype == BF16 else 4
+    ld, n, n_in, n_out = 1 << 29, 5, 24, 6
+    if torch.cuda.mem_get_info()[0] < 3 * 6 * ld * e:
+        pytest.skip("not enough memory")
+    rng = np.random.default_rng(8)
+    big = torch.empty(6 * ld, dtype=dtype, device=DEV)
+    view = lambda at, rows, cols: torch.as_strided(big, (rows, cols), (ld, 1), at)
+    x, w, y, dx = view(0, n, n_in), view(64, n_out, n_in), view(128, n, n_out), view(192, n, n_in)
+    hx, hw = rng.normal(size=(n, n_in)), rng.normal(size=(n_out, n_in))
+    x.copy_(torch.from_numpy(hx))
+    w.copy_(torch.from_numpy(hw))
+    op = layer(n_in, n_out, dtype, "none", n)
+    op.forward(x, w, y)
+    want = ref.dense(host(x), host(w))[0]
+    close(y, want, forward_tol(host(x), host(w), None, None, want, dtype, n_in)[1])
+    dw = like((n_out, n_in))
+    op.backward(x, w, y, dx=dx, dw=dw)
+    hx, hw, hy = host(x), host(w), host(y)
+    want = ref.dense_back(hx, hw, hy)
+    tol = backward_tols(hx, hw, hy, None, "none", n_out, n)
+    close(dx, want[0], tol[0] + half(dtype) * np.abs(want[0]))
+    close(dw, want[1], tol[1] + U * np.abs(want[1]))
+    op.close()
