@@ -20,14 +20,13 @@ struct SlopeArgs {
   void* dz;                 // rows of lddz values, planes plane_stride elements apart
   int64_t lddz, plane_stride;
   int64_t n, cols;
-  int32_t act;
   float* sums;              // [chunk][cols] (nullable)
   ColumnPlan plan;
 };
 
 // dz = dy act'(pre) and its column sums.  PLANES: what is written of dz (0: nothing, dz is dy): one matrix, or in
 // bf16 the three terms whose sum is dz in 24 bits.
-template <class T, int PLANES>
+template <class T, int PLANES, int ACT>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
   __shared__ float s[256][9];
   const int w = a.plan.col_threads, cx = threadIdx.x % w, rx = threadIdx.x / w, lanes = 256 / w;
@@ -43,7 +42,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
         float z[8];
         load8(static_cast<const T*>(a.pre) + r * a.ldp + c, a.cols - c, z);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_back(v[e], z[e], a.act);
+        for (int e = 0; e < 8; ++e) v[e] = act_back<ACT>(v[e], z[e]);
         T* out = static_cast<T*>(a.dz) + r * a.lddz + c;
         if constexpr (PLANES == 3) {
           lr_u32x4 t[3];
@@ -119,18 +118,16 @@ int run_product(ot::Product p, const ot_dense* d, const ot::ProductArgs& a, hipS
   return d->precision == OT_BF16 ? ot::run_product_bf16(p, a, st) : ot::run_product_f32(p, a, st);
 }
 
-int run_slope(const ot_dense* d, ot::SlopeArgs a, int planes, float* dbias, float* part, hipStream_t st) {
+int run_slope(const ot_dense* d, ot::SlopeArgs a, float* dbias, float* part, hipStream_t st) {
   a.plan = ot::plan_columns(a.n, a.cols);
   a.sums = dbias ? (a.plan.chunks > 1 ? part : dbias) : nullptr;
   const dim3 grid((unsigned)a.plan.blocks_x, (unsigned)a.plan.chunks), block(256);
-  if (d->precision == OT_FP32) {
-    if (planes) hipLaunchKernelGGL((ot::slope_kernel<float, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((ot::slope_kernel<float, 0>), grid, block, 0, st, a);
-  } else {
-    if (planes == 3) hipLaunchKernelGGL((ot::slope_kernel<uint16_t, 3>), grid, block, 0, st, a);
-    else if (planes) hipLaunchKernelGGL((ot::slope_kernel<uint16_t, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((ot::slope_kernel<uint16_t, 0>), grid, block, 0, st, a);
-  }
+  ot::with_act(d->act, [&](auto act) {
+    constexpr int A = decltype(act)::value;
+    constexpr int PLANES = A == ot::kActNone ? 0 : 1, TERMS = A == ot::kActNone ? 0 : A == ot::kActRelu ? 1 : 3;
+    if (d->precision == OT_FP32) hipLaunchKernelGGL((ot::slope_kernel<float, PLANES, A>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((ot::slope_kernel<uint16_t, TERMS, A>), grid, block, 0, st, a);
+  });
   OT_LAUNCHED("slope_kernel");
   if (dbias && a.plan.chunks > 1) {
     hipLaunchKernelGGL(ot::column_join_kernel, dim3((unsigned)ot::ceil_div(a.cols, 64)), dim3(1024), 0, st, part,
@@ -236,8 +233,8 @@ extern "C" int dense_backward(ot_dense* d, const void* x, int64_t ldx, const voi
   void* dz = sz.planes ? d->ws.p : const_cast<void*>(dy);
   float* part = reinterpret_cast<float*>(d->ws.p + ot::dz_bytes(sz, n));
   if (sz.planes || dbias) {
-    const ot::SlopeArgs s{dy, lddy, pre, ldp, dz, ldz, n * ldz, n, d->out, d->act, nullptr, {}};
-    if ((rc = run_slope(d, s, sz.planes, dbias, part, st))) return rc;
+    const ot::SlopeArgs s{dy, lddy, pre, ldp, dz, ldz, n * ldz, n, d->out, nullptr, {}};
+    if ((rc = run_slope(d, s, dbias, part, st))) return rc;
   }
   ot::LayerArgs ly{};
   ly.planes = std::max(1, sz.planes);

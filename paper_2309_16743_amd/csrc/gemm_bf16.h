@@ -417,10 +417,7 @@ struct BEpi {
           else
             for (int c = 0; c < cnt; ++c) P[c] = h[c];
         }
-        if (g.ly.act != kActNone) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) v[c] = act_value(v[c], g.ly.act);
-        }
+        act_values<4>(v, g.ly.act);
         v += res[u];
         if constexpr (EPI == EpiB::LayerF32) {
           float* C = reinterpret_cast<float*>(g.C) + m * g.ldc + col;

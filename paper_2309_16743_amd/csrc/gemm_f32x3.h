@@ -739,8 +739,9 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
 #pragma unroll
           for (int h = 0; h < FN; ++h) val[h] = acc[f][h][r0 + u] + bias[h];
           if (g.ly.pre) put(static_cast<float*>(g.ly.pre) + m * g.ly.ldp, val);
+          act_values<FN>(val, g.ly.act);
 #pragma unroll
-          for (int h = 0; h < FN; ++h) val[h] = act_value(val[h], g.ly.act) + res[u][h];
+          for (int h = 0; h < FN; ++h) val[h] += res[u][h];
           if constexpr (BF) {
             uint16_t* C = reinterpret_cast<uint16_t*>(g.C) + m * g.ldc;
             if (IL && full) {

@@ -29,6 +29,35 @@ inline int32_t slab_groups(const NormSizes& s) {
   return (int32_t)fit;
 }
 
+// Lanes that keep a sample's group in registers (0: it has no whole vectors of 8 channels, or more than 4
+// of them a lane), and how many vectors each holds.
+inline int32_t team_lanes(const NormSizes& s) {
+  const int64_t vecs = s.per() / 8 * s.positions;
+  if (s.per() % 8 != 0 || vecs > 4 * 64) return 0;
+  int32_t lanes = 1;
+  while (lanes < 64 && lanes < vecs) lanes *= 2;
+  return lanes;
+}
+inline int32_t team_vectors(const NormSizes& s) {
+  const int64_t v = ceil_div(s.per() / 8 * s.positions, team_lanes(s));
+  return v > 2 ? 4 : (int32_t)v;
+}
+
+// The backward over teams (one position): a block takes `groups` groups, tiles of them cover a sample, in
+// `ranges` of the samples.
+struct TeamPlan {
+  int32_t lanes, groups;
+  int64_t tiles, ranges;
+};
+constexpr int64_t kTeamBlocks = 256;
+inline TeamPlan plan_team_back(const NormSizes& s, int64_t n) {
+  TeamPlan t{team_lanes(s), 1, 0, 0};
+  while (t.groups * 2 <= s.groups && t.groups * 2 * t.lanes <= 256) t.groups *= 2;
+  t.tiles = ceil_div(s.groups, t.groups);
+  t.ranges = std::max<int64_t>(1, std::min(ceil_div(n, 256 / t.lanes / t.groups), kTeamBlocks / t.tiles));
+  return t;
+}
+
 // Split passes: a block holds col_threads x 8 channels (tiles of them cover the row) and a chunk of `rows`
 // positions of one sample.
 struct NormPlan {

@@ -234,3 +234,34 @@ def test_row_offsets_past_32_bits(dtype):
     close(dx, want[0], tol[0] + half(dtype) * np.abs(want[0]))
     close(dw, want[1], tol[1] + U * np.abs(want[1]))
     op.close()
+
+
+@pytest.mark.parametrize("name", ACTS)
+def test_activations_and_slopes(name):
+    """A layer of one weight 1 is the activation itself, its input gradient the slope: over the range where gelu's
+    lower tail is a normal number, at the corner, and where exp over- or underflows."""
+    z = np.concatenate([np.linspace(-12.5, 12.5, 20001), [0.0, -0.0, 1e-30, -1e-30, 80, -80, 87.5, -87.5, 1e4, -1e4, 3e38]])
+    x, one = padded(z[:, None]), padded(np.ones((1, 1)))
+    hx = host(x)
+    n = len(z)
+    y, dx = like((n, 1)), like((n, 1))
+    op = layer(1, 1, F32, name, n)
+    op.forward(x, one, y)
+    op.backward(x, one, padded(np.ones((n, 1))), pre=x, dx=dx)
+    want, slope = ref.act(hx, name), ref.slope(hx, name)
+    # Phi is off by 7 u of its value, the sigmoid by 4, the products by 2; a slope adds z phi(z), of size 0.25 and
+    # off by 6 u, or z s (1 - s), where 1 - s is off by u.  Sigmoids and integrals below 2^-126, the smallest normal
+    # number, are taken as 0 (the device's reciprocal and exp2 have no smaller results), times |z| in y and slope.
+    none = np.minimum(np.abs(hx), 200) * 2.0 ** -126
+    close(y, want, 10 * U * np.abs(want) + none, "y")
+    close(dx, slope, 10 * U * (np.abs(slope) + 0.3) + none if name in ("silu", "gelu") else 0, "slope")
+    # NaN, and infinities as the formula has them
+    x = padded(np.array([[np.nan], [np.inf], [-np.inf]]))
+    y = like((3, 1))
+    op.forward(x, one, y)
+    with np.errstate(invalid="ignore"):
+        want = ref.act(host(x), name)
+    got = host(y)
+    assert np.isnan(got[0, 0]) and got[1, 0] == np.inf
+    assert name in ("silu", "gelu") or got[2, 0] == want[2, 0]
+    op.close()
