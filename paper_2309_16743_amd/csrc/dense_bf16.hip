@@ -9,18 +9,28 @@ namespace {
 
 constexpr LayB KM = LayB::KMajor, MN = LayB::MNMajor;
 
-// The tiles that the plans give for each product.
-template <LayB LA, LayB LB, EpiB E>
+// The tiles that plan_dense gives for each product, whole or split.
+template <Product P, EpiB E>
 hipError_t launch(int tile, const GemmBArgs& g, int64_t splits, hipStream_t st) {
-  if constexpr (LB == KM) {
-    if (tile == kB64x64) return launch_gemm_bf16_pipe<64, 64, 64, 4, 2, LA, LB, E>(g, splits, st);
+  constexpr LayB LA = P == Product::WeightGrad ? MN : KM, LB = P == Product::Forward ? KM : MN;
+  constexpr bool split = E == EpiB::LayerSplit;
+  if constexpr (P == Product::Forward) {
+    if (tile == kT64x64) return launch_gemm_bf16_pipe<64, 64, 64, 4, 2, LA, LB, E>(g, splits, st);
   }
-  if constexpr (LA == KM) {
-    if (tile == kB64x128) return launch_gemm_bf16_pipe<64, 128, 64, 3, 4, LA, LB, E, 4>(g, splits, st);
+  if constexpr (P != Product::WeightGrad) {
+    if (tile == kT64x128) return launch_gemm_bf16_pipe<64, 128, 64, 3, 4, LA, LB, E, 4>(g, splits, st);
   }
-  if (tile == kB128x128) return launch_gemm_bf16_pipe<128, 128, 32, 4, 2, LA, LB, E>(g, splits, st);
-  if constexpr (!(LA == MN && E == EpiB::LayerSplit)) {
-    if (tile == kB256x256) return launch_gemm_bf16_pp<4, LA, LB, E>(g, splits, st);
+  if constexpr (!split) {
+    if (tile == kT128k32) return launch_gemm_bf16_pipe<128, 128, 32, 3, 3, LA, LB, E>(g, splits, st);
+  }
+  if constexpr (P == Product::InputGrad && !split) {
+    if (tile == kT128k64) return launch_gemm_bf16_pipe<128, 128, 64, 2, 2, LA, LB, E>(g, splits, st);
+  }
+  if constexpr (P != Product::Forward) {
+    if (tile == kT128w8) return launch_gemm_bf16_pipe<128, 128, 64, 2, 2, LA, LB, E, 4>(g, splits, st);
+  }
+  if constexpr (!(P == Product::WeightGrad && split)) {
+    if (tile == kT256) return launch_gemm_bf16_pp<4, LA, LB, E>(g, splits, st);
   }
   return hipErrorInvalidValue;
 }
@@ -28,8 +38,7 @@ hipError_t launch(int tile, const GemmBArgs& g, int64_t splits, hipStream_t st) 
 }  // namespace
 
 int run_product_bf16(Product p, const ProductArgs& a, hipStream_t st) {
-  const AdaptPlan plan = p == Product::WeightGrad ? plan_wgrad(true, a.M, a.N, a.K)
-                                                  : plan_expand(true, p == Product::Forward, a.M, a.N, a.K);
+  const AdaptPlan plan = split_dense(plan_dense(true, p, a.M, a.N, a.K, a.ly.planes), a.K);
   GemmBArgs g{};
   g.A = static_cast<const uint16_t*>(a.A);
   g.lda = a.lda;
@@ -51,14 +60,14 @@ int run_product_bf16(Product p, const ProductArgs& a, hipStream_t st) {
   }
   hipError_t rc;
   if (p == Product::Forward)
-    rc = a.c_type == OT_BF16 ? launch<KM, KM, EpiB::LayerBf>(plan.tile, g, 1, st)
-                             : launch<KM, KM, EpiB::LayerF32>(plan.tile, g, 1, st);
+    rc = a.c_type == OT_BF16 ? launch<Product::Forward, EpiB::LayerBf>(plan.tile, g, 1, st)
+                             : launch<Product::Forward, EpiB::LayerF32>(plan.tile, g, 1, st);
   else if (p == Product::InputGrad)
-    rc = split ? launch<KM, MN, EpiB::LayerSplit>(plan.tile, g, plan.splits, st)
-               : launch<KM, MN, EpiB::LayerBf>(plan.tile, g, 1, st);
+    rc = split ? launch<Product::InputGrad, EpiB::LayerSplit>(plan.tile, g, plan.splits, st)
+               : launch<Product::InputGrad, EpiB::LayerBf>(plan.tile, g, 1, st);
   else
-    rc = split ? launch<MN, MN, EpiB::LayerSplit>(plan.tile, g, plan.splits, st)
-               : launch<MN, MN, EpiB::LayerF32>(plan.tile, g, 1, st);
+    rc = split ? launch<Product::WeightGrad, EpiB::LayerSplit>(plan.tile, g, plan.splits, st)
+               : launch<Product::WeightGrad, EpiB::LayerF32>(plan.tile, g, 1, st);
   if (rc != hipSuccess)
     return set_error(OT_E_HIP, "launch of the dense product failed: %s", hipGetErrorString(rc));
   if (!split) return OT_OK;

@@ -9,18 +9,23 @@ namespace {
 
 constexpr Lay KM = Lay::KMajor, MN = Lay::MNMajor;
 
-// The tiles that the plans give for each product.
-template <Lay LA, Lay LB, Epi E>
+// The tiles that plan_dense gives for each product, whole or split.
+template <Product P, Epi E>
 hipError_t launch(int tile, const GemmArgs& g, int64_t splits, hipStream_t st) {
-  if (tile == kX64x64) return launch_gemm_f32x3<2, 2, 1, 1, LA, LB, E>(g, splits, st);
-  if constexpr (LA == KM) {
-    if (tile == kX32x256) return launch_gemm_f32x3<1, 4, 1, 2, LA, LB, E>(g, splits, st);
-    if (tile == kX64x256) return launch_gemm_f32x3<1, 4, 2, 2, LA, LB, E>(g, splits, st);
+  constexpr Lay LA = P == Product::WeightGrad ? MN : KM, LB = P == Product::Forward ? KM : MN;
+  constexpr bool split = E == Epi::SplitK;
+  if (tile == kF64x64) return launch_gemm_f32x3<2, 2, 1, 1, LA, LB, E>(g, splits, st);
+  if constexpr (P != Product::WeightGrad) {
+    if (tile == kF32x256) return launch_gemm_f32x3<1, 4, 1, 2, LA, LB, E>(g, splits, st);
+    if (tile == kF64x256) return launch_gemm_f32x3<1, 4, 2, 2, LA, LB, E>(g, splits, st);
   }
-  if constexpr (LB == KM) {
-    if (tile == kX64x128) return launch_gemm_f32x3<2, 2, 1, 2, LA, LB, E>(g, splits, st);
-  } else {
-    if (tile == kX128x128) return launch_gemm_f32x3<2, 2, 2, 2, LA, LB, E>(g, splits, st);
+  if constexpr (P == Product::Forward) {
+    if (tile == kF64x128) return launch_gemm_f32x3<2, 2, 1, 2, LA, LB, E>(g, splits, st);
+  } else if constexpr (!(P == Product::WeightGrad && split)) {
+    if (tile == kF128x128) return launch_gemm_f32x3<2, 2, 2, 2, LA, LB, E>(g, splits, st);
+  }
+  if constexpr (P == Product::WeightGrad) {
+    if (tile == kF128x64) return launch_gemm_f32x3<4, 1, 1, 2, LA, LB, E>(g, splits, st);
   }
   return hipErrorInvalidValue;
 }
@@ -28,8 +33,7 @@ hipError_t launch(int tile, const GemmArgs& g, int64_t splits, hipStream_t st) {
 }  // namespace
 
 int run_product_f32(Product p, const ProductArgs& a, hipStream_t st) {
-  const AdaptPlan plan = p == Product::WeightGrad ? plan_wgrad(false, a.M, a.N, a.K)
-                                                  : plan_expand(false, p == Product::Forward, a.M, a.N, a.K);
+  const AdaptPlan plan = split_dense(plan_dense(false, p, a.M, a.N, a.K, 1), a.K);
   GemmArgs g{};
   g.A = static_cast<const float*>(a.A);
   g.lda = a.lda;
@@ -51,14 +55,14 @@ int run_product_f32(Product p, const ProductArgs& a, hipStream_t st) {
   }
   hipError_t rc;
   if (p == Product::Forward)
-    rc = a.c_type == OT_BF16 ? launch<KM, KM, Epi::LayerBf>(plan.tile, g, 1, st)
-                             : launch<KM, KM, Epi::LayerF32>(plan.tile, g, 1, st);
+    rc = a.c_type == OT_BF16 ? launch<Product::Forward, Epi::LayerBf>(plan.tile, g, 1, st)
+                             : launch<Product::Forward, Epi::LayerF32>(plan.tile, g, 1, st);
   else if (p == Product::InputGrad)
-    rc = split ? launch<KM, MN, Epi::SplitK>(plan.tile, g, plan.splits, st)
-               : launch<KM, MN, Epi::Store>(plan.tile, g, 1, st);
+    rc = split ? launch<Product::InputGrad, Epi::SplitK>(plan.tile, g, plan.splits, st)
+               : launch<Product::InputGrad, Epi::Store>(plan.tile, g, 1, st);
   else
-    rc = split ? launch<MN, MN, Epi::SplitK>(plan.tile, g, plan.splits, st)
-               : launch<MN, MN, Epi::Store>(plan.tile, g, 1, st);
+    rc = split ? launch<Product::WeightGrad, Epi::SplitK>(plan.tile, g, plan.splits, st)
+               : launch<Product::WeightGrad, Epi::Store>(plan.tile, g, 1, st);
   if (rc != hipSuccess)
     return set_error(OT_E_HIP, "launch of the dense product failed: %s", hipGetErrorString(rc));
   return split ? join_splits<float>(a, plan.splits, g.split_stride, g.ldc, st) : OT_OK;

@@ -5,13 +5,12 @@
 
 #include "common.h"
 #include "layer_ops.h"
+#include "layer_plan.h"
 
 namespace ot {
 
-// C = A B^T over K: the layer (A = x, B = W, both KMajor), its input gradient (A = dz KMajor, B = W MNMajor)
-// or its weight gradient (A = dz, B = x, both MNMajor).
-enum class Product : int { Forward, InputGrad, WeightGrad };
-
+// C = A B^T over K.  Forward: the layer (A = x, B = W, both KMajor); InputGrad: A = dz KMajor, B = W MNMajor;
+// WeightGrad: A = dz, B = x, both MNMajor.
 struct ProductArgs {
   const void* A;
   int64_t lda;

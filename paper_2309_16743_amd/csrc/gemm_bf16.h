@@ -220,10 +220,6 @@ struct BEpi {
       adapt_rows<NP>(g, ep, m0, split, stage);
       return;
     }
-    if constexpr (is_layer(EPI)) {
-      layer_rows<NP>(g, ep, m0, split, stage);
-      return;
-    }
     // targets (MseBf) or mask (MaskBf) of each pass; one branch around all
     // the loads of the chunk, so that they are all in flight together
     f32x4 pre[NP];
@@ -364,14 +360,28 @@ struct BEpi {
     }
   }
 
-  // Layer*: the residuals of G passes are read together.  Rows are padded to whole 16-byte pieces,
-  // so 4 columns are read together if one exists; a lane reads its residuals before it writes the same
-  // columns of C, which may be the residual itself.
-  template <int NP, class Stage>
-  __device__ __forceinline__ void layer_rows(const GemmBArgs& g, const float* ep, int64_t m0, int64_t split,
-                                             Stage stage) {
-    constexpr int G = NP < 4 ? NP : 4;
-    static_assert(NP % G == 0, "pass groups");
+  // Layer*: passes are taken in groups of G, whose residuals are read before the group ahead of them writes: loads
+  // and stores complete in order, so a load behind a store would wait for it (160000 x 256 x 256 with residual and
+  // pre: 104 us with each group's loads behind the last one's stores).  Rows are padded to
+  // whole 16-byte pieces, so 4 columns are read together if one exists; C may be the residual itself: a lane
+  // reads every residual before it writes those columns.
+  static constexpr int LG = 4;
+  typedef typename std::conditional<EPI == EpiB::LayerF32, f32x4, u16x4>::type Res;
+  Res ahead[LG];
+  __device__ __forceinline__ void layer_ahead(const GemmBArgs& g, int64_t row0) {
+    typedef typename std::conditional<EPI == EpiB::LayerF32, float, uint16_t>::type E;
+    if (!g.ly.residual || col >= g.N) return;
+#pragma unroll
+    for (int u = 0; u < LG; ++u)
+      ahead[u] = *reinterpret_cast<const Res*>(static_cast<const E*>(g.ly.residual) +
+                                               min(row0 + rl + RPP * u, g.M - 1) * g.ly.ldr + col);
+  }
+  // next: row 0 of the wavefront's next chunk (-1: none)
+  template <int ROWS, class Stage>
+  __device__ __forceinline__ void layer_rows(const GemmBArgs& g, const float* ep, int64_t m0, int64_t next,
+                                             int64_t split, Stage stage) {
+    constexpr int NP = ROWS / RPP;
+    static_assert(NP % LG == 0, "pass groups");
     stage();
     if (col >= g.N) return;
     if constexpr (EPI == EpiB::LayerSplit) {
@@ -386,24 +396,14 @@ struct BEpi {
     }
     const int cnt = (int)min((int64_t)4, g.N - col);
 #pragma unroll 1
-    for (int i0 = 0; i0 < NP; i0 += G) {
-      f32x4 res[G];
+    for (int i0 = 0; i0 < NP; i0 += LG) {
+      Res res[LG];
 #pragma unroll
-      for (int u = 0; u < G; ++u) {
-        res[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int64_t m = min(m0 + rl + RPP * (i0 + u), g.M - 1);
-        if (g.ly.residual) {
-          if constexpr (EPI == EpiB::LayerF32) {
-            res[u] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(g.ly.residual) + m * g.ly.ldr + col);
-          } else {
-            const u16x4 h =
-                *reinterpret_cast<const u16x4*>(static_cast<const uint16_t*>(g.ly.residual) + m * g.ly.ldr + col);
-            res[u] = f32x4{bf2f(h[0]), bf2f(h[1]), bf2f(h[2]), bf2f(h[3])};
-          }
-        }
-      }
+      for (int u = 0; u < LG; ++u) res[u] = ahead[u];
+      if (i0 + LG < NP) layer_ahead(g, m0 + RPP * (i0 + LG));
+      else if (next >= 0) layer_ahead(g, next);
 #pragma unroll
-      for (int u = 0; u < G; ++u) {
+      for (int u = 0; u < LG; ++u) {
         const int rr = rl + RPP * (i0 + u);
         const int64_t m = m0 + rr;
         if (m >= g.M) continue;
@@ -418,10 +418,13 @@ struct BEpi {
             for (int c = 0; c < cnt; ++c) P[c] = h[c];
         }
         act_values<4>(v, g.ly.act);
-        v += res[u];
+        if (g.ly.residual) {
+          if constexpr (EPI == EpiB::LayerF32) v += res[u];
+          else v += f32x4{bf2f(res[u][0]), bf2f(res[u][1]), bf2f(res[u][2]), bf2f(res[u][3])};
+        }
         if constexpr (EPI == EpiB::LayerF32) {
           float* C = reinterpret_cast<float*>(g.C) + m * g.ldc + col;
-          if (cnt == 4) *reinterpret_cast<f32x4*>(C) = v;
+          if (cnt == 4) __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(C));
           else
             for (int c = 0; c < cnt; ++c) C[c] = v[c];
         } else {
@@ -1337,9 +1340,11 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
     e.tile_m0 = m0;
     e.odd = odd;
   }
+  if constexpr (is_layer(EPI)) e.layer_ahead(g, m0 + WM * wm);
 #pragma unroll
   for (int c0 = 0; c0 < FM; c0 += CH_F) {
-    e.template rows<CH_F * 32>(g, ep, m0 + WM * wm + 32 * c0, split, [&] {
+    const int64_t mc = m0 + WM * wm + 32 * c0;
+    auto stage = [&] {
       lds_barrier();                  // other waves are done with the stage buffers / previous chunk
 #pragma unroll
       for (int f = 0; f < CH_F; ++f)
@@ -1349,7 +1354,11 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
           for (int r = 0; r < 16; ++r)
             ep[(32 * f + 8 * (r / 4) + 4 * (lane / 32) + r % 4) * EP + 32 * h + lane % 32] = acc[c0 + f][h][r];
       lds_barrier();
-    });
+    };
+    if constexpr (is_layer(EPI))
+      e.template layer_rows<CH_F * 32>(g, ep, mc, c0 + CH_F < FM ? mc + 32 * CH_F : -1, split, stage);
+    else
+      e.template rows<CH_F * 32>(g, ep, mc, split, stage);
   }
   e.finish(g, tm, s_red);
 }
@@ -1532,9 +1541,11 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
     e.tile_m0 = m0;
     e.odd = odd;
   }
+  if constexpr (is_layer(EPI)) e.layer_ahead(g, m0 + WM * wm);
 #pragma unroll
   for (int c0 = 0; c0 < FM; c0 += CH_F) {
-    e.template rows<CH_F * 32>(g, ep, m0 + WM * wm + 32 * c0, split, [&] {
+    const int64_t mc = m0 + WM * wm + 32 * c0;
+    auto stage = [&] {
       lds_barrier();
 #pragma unroll
       for (int f = 0; f < CH_F; ++f)
@@ -1544,7 +1555,11 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
           for (int r = 0; r < 16; ++r)
             ep[(32 * f + 8 * (r / 4) + 4 * (lane / 32) + r % 4) * EP + 32 * h + lane % 32] = acc[c0 + f][h][r];
       lds_barrier();
-    });
+    };
+    if constexpr (is_layer(EPI))
+      e.template layer_rows<CH_F * 32>(g, ep, mc, c0 + CH_F < FM ? mc + 32 * CH_F : -1, split, stage);
+    else
+      e.template rows<CH_F * 32>(g, ep, mc, split, stage);
   }
   e.finish(g, tm, s_red);
 }

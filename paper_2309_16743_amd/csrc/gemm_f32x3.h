@@ -709,28 +709,39 @@ __global__ __launch_bounds__(256, x3_waves(WGN, FM, FN)) void gemm_f32x3_kernel(
     constexpr bool BF = EPI == Epi::LayerBf;
 #pragma unroll
     for (int h = 0; h < FN; ++h) bias[h] = g.bias && col_of(h) < g.N ? g.bias[col_of(h)] : 0.f;
-    // residuals of four rows are read together, before the lane writes the same columns of C, which may be the
-    // residual itself
+    // residuals of four rows are read together, ahead of the writes of the four rows before them (a load behind
+    // a store waits for it); C may be the residual itself: a lane reads every residual before it writes those columns
+    float ahead[4][FN];
+    auto load_ahead = [&](int f, int r0) {
+      if (!g.ly.residual) return;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t m = min(row_of(f, r0 + u), g.M - 1);
+        if constexpr (BF) {
+          const uint16_t* p = static_cast<const uint16_t*>(g.ly.residual) + m * g.ly.ldr;
+#pragma unroll
+          for (int h = 0; h < FN; ++h) ahead[u][h] = col_of(h) < g.N ? lr_value(p + col_of(h)) : 0.f;
+        } else {
+          get(static_cast<const float*>(g.ly.residual) + m * g.ly.ldr, ahead[u]);
+        }
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int h = 0; h < FN; ++h) ahead[u][h] = 0.f;
+    load_ahead(0, 0);
 #pragma unroll
     for (int f = 0; f < FM; ++f)
 #pragma unroll
       for (int r0 = 0; r0 < 16; r0 += 4) {
         float res[4][FN];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int64_t m = min(row_of(f, r0 + u), g.M - 1);
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-          for (int h = 0; h < FN; ++h) res[u][h] = 0.f;
-          if (!g.ly.residual) continue;
-          if constexpr (BF) {
-            const uint16_t* p = static_cast<const uint16_t*>(g.ly.residual) + m * g.ly.ldr;
-#pragma unroll
-            for (int h = 0; h < FN; ++h)
-              if (col_of(h) < g.N) res[u][h] = lr_value(p + col_of(h));
-          } else {
-            get(static_cast<const float*>(g.ly.residual) + m * g.ly.ldr, res[u]);
-          }
-        }
+          for (int h = 0; h < FN; ++h) res[u][h] = ahead[u][h];
+        if (r0 + 4 < 16) load_ahead(f, r0 + 4);
+        else if (f + 1 < FM) load_ahead(f + 1, 0);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int64_t m = row_of(f, r0 + u);
