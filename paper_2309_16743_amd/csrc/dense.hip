@@ -34,28 +34,31 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
   const int64_t r0 = (int64_t)blockIdx.y * a.plan.rows, r1 = min(a.n, r0 + a.plan.rows);
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (c < a.cols) {
-#pragma unroll 2
-    for (int64_t r = r0 + rx; r < r1; r += lanes) {
-      float v[8];
-      load8(static_cast<const T*>(a.dy) + r * a.lddy + c, a.cols - c, v);
-      if constexpr (PLANES > 0) {
-        float z[8];
-        load8(static_cast<const T*>(a.pre) + r * a.ldp + c, a.cols - c, z);
+    constexpr int U = 4;
+    float v[U][8], z[U][8];
+    rows_in_groups<U>(
+        r0 + rx, r1, lanes,
+        [&](int u, int64_t r) {
+          load8(static_cast<const T*>(a.dy) + r * a.lddy + c, a.cols - c, v[u]);
+          if constexpr (PLANES > 0) load8(static_cast<const T*>(a.pre) + r * a.ldp + c, a.cols - c, z[u]);
+        },
+        [&](int u, int64_t r) {
+          if constexpr (PLANES > 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_back<ACT>(v[e], z[e]);
-        T* out = static_cast<T*>(a.dz) + r * a.lddz + c;
-        if constexpr (PLANES == 3) {
-          lr_u32x4 t[3];
-          lr_split8(v, t);
+            for (int e = 0; e < 8; ++e) v[u][e] = act_back<ACT>(v[u][e], z[u][e]);
+            T* out = static_cast<T*>(a.dz) + r * a.lddz + c;
+            if constexpr (PLANES == 3) {
+              lr_u32x4 t[3];
+              lr_split8(v[u], t);
 #pragma unroll
-          for (int p = 0; p < 3; ++p) *reinterpret_cast<lr_u32x4*>(out + p * a.plane_stride) = t[p];
-        } else {
-          store8(out, 8, v);                             // (rows of dz are padded to 8 values)
-        }
-      }
+              for (int p = 0; p < 3; ++p) *reinterpret_cast<lr_u32x4*>(out + p * a.plane_stride) = t[p];
+            } else {
+              store8(out, 8, v[u]);                      // (rows of dz are padded to 8 values)
+            }
+          }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += v[e];
-    }
+          for (int e = 0; e < 8; ++e) sum[e] += v[u][e];
+        });
   }
   if (!a.sums) return;
 #pragma unroll

@@ -51,6 +51,7 @@ struct DensePlan {
 // fp32 weight gradients: 6561 x 437 over 331 rows on 64 x 64, 128 x 128, 128 x 64 in 2: 38.6, 41.9, 35.5; 10000 x
 //   256 over 1024 rows on 128 x 128 in 4, 128 x 64 in 1, 2, 4: 62, 98, 67, 59; 2048 x 2048 over 1024 on 128 x 128,
 //   128 x 64: 56, 62; 256 x 256 over 1024 on 64 x 64, 128 x 64 in 4: 13.9, 17.8.
+constexpr int64_t kLongRows = 768;
 inline DensePlan plan_dense(bool bf16, Product product, int64_t M, int64_t N, int64_t K, int planes) {
   constexpr int64_t kCUs = 256;
   auto tiles = [&](int t) { return dense_tiles(t, M, N); };
@@ -86,7 +87,7 @@ inline DensePlan plan_dense(bool bf16, Product product, int64_t M, int64_t N, in
       if (M > 64 && N > 64 && K >= 1024) return {kF128x128, splits(2 * kCUs / tiles(kF128x128), K / 128)};
       return {kF64x64, splits(2 * kCUs / tiles(kF64x64), K / 64)};
     default:
-      if (N > 64 && tiles(kF128x128) >= 200) return {kF128x128, 1};
+      if (N > 64 && K >= kLongRows && tiles(kF128x128) >= 200) return {kF128x128, 1};
       if (tiles(kF64x64) > 256) return {kF128x64, splits(5 * kCUs / tiles(kF128x64), K / 160)};
       return {kF64x64, splits(2 * kCUs / tiles(kF64x64), K / 128)};
   }
@@ -146,8 +147,8 @@ inline int64_t dense_values(const DenseSizes& d, int64_t n) {
   if (n < 1) return 0;
   // column sums: chunks * blocks_x <= kColumnBlocks
   int64_t most = std::min(kColumnBlocks * 256 * 8, ceil_div(n, 4) * d.out);
-  // the weight gradient: where it is split, the tile is the same and the splits asked for grow with the rows
-  most = std::max(most, dw_values(d, n));
+  // the weight gradient: the tile changes at kLongRows only, and the splits asked for grow with the rows
+  most = std::max(most, std::max(dw_values(d, n), dw_values(d, std::min(n, kLongRows - 1))));
   // the input gradient: a plan depends on the rows only through whole groups of 32, and past 65536 of them
   // there are so many tiles that nothing is split
   for (int64_t m = 32; m < std::min<int64_t>(n, 65536) + 32; m += 32) most = std::max(most, dx_values(d, m));

@@ -94,7 +94,8 @@ __global__ __launch_bounds__(256) void norm_team_kernel(NormArgs a, int S) {
   for (int64_t t0 = (int64_t)blockIdx.x * (256 / S); t0 < teams; t0 += (int64_t)gridDim.x * (256 / S)) {
     const int64_t q = t0 + threadIdx.x / S;
     const bool in = q < teams;
-    const int64_t s = in ? q / a.groups : 0, g = in ? q % a.groups : 0;
+    int64_t g;
+    const int64_t s = quotient(in ? q : 0, a.groups, g);
     float v[V][8];
     int64_t at[V];                                       // row, channel of each vector
     int ch[V];
@@ -471,12 +472,11 @@ __global__ __launch_bounds__(256) void norm_slab_back_kernel(NormArgs a, int gb,
 
 // Where block b of a split pass stands.
 struct NormSpot {
-  int64_t sample, chunk, r0, r1, c;      // rows r0 .. r1 of the data; this thread's first channel
+  int64_t tile, sample, chunk, r0, r1, c;      // rows r0 .. r1 of the data; this thread's first channel
   int rx, lanes;                         // its row among those side by side
   __device__ __forceinline__ NormSpot(const NormArgs& a, const NormPlan& p, int64_t b) {
-    const int64_t tile = b % p.tiles, q = b / p.tiles;
-    sample = q / p.chunks;
-    chunk = q % p.chunks;
+    const int64_t q = quotient(b, p.tiles, tile);
+    sample = quotient(q, p.chunks, chunk);
     lanes = 256 / p.col_threads;
     rx = threadIdx.x / p.col_threads;
     c = 8 * (tile * p.col_threads + threadIdx.x % p.col_threads);
@@ -508,24 +508,21 @@ __global__ __launch_bounds__(256) void norm_moments_kernel(NormArgs a, NormPlan 
     int mine = 0;
     if (left > 0) {
       const T* x = static_cast<const T*>(a.x) + at.c;
-      int64_t r = at.r0 + at.rx;
-      if (r < at.r1) {
-        load8(x + r * a.ldx, left, first);
-        mine = 1;
-        r += at.lanes;
-      }
-#pragma unroll 4
-      for (; r < at.r1; r += at.lanes) {
-        float v[8];
-        load8(x + r * a.ldx, left, v);
-        ++mine;
+      const int64_t r0 = at.r0 + at.rx;
+      if (r0 < at.r1) load8(x + r0 * a.ldx, left, first);
+      constexpr int U = 4;
+      float v[U][8];
+      rows_in_groups<U>(
+          r0, at.r1, at.lanes, [&](int u, int64_t r) { load8(x + r * a.ldx, left, v[u]); },
+          [&](int u, int64_t) {
+            ++mine;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float d = v[e] - first[e];
-          s1[e] += d;
-          s2[e] = fmaf(d, d, s2[e]);
-        }
-      }
+            for (int e = 0; e < 8; ++e) {
+              const float d = v[u][e] - first[e];
+              s1[e] += d;
+              s2[e] = fmaf(d, d, s2[e]);
+            }
+          });
     }
     const float inv = mine > 0 ? 1.f / (float)mine : 0.f;
 #pragma unroll
@@ -562,40 +559,42 @@ __global__ __launch_bounds__(256) void norm_moments_kernel(NormArgs a, NormPlan 
   }
 }
 
-// Block per sample and group: mean and rstd from the partial moments, in 64 bits.
-__global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a, NormPlan p, const float* part, float* stats) {
+// Sums over a group's partial values in 64 bits by a whole block: f(chunk, channel, u, v) adds to u and v.
+template <class F>
+__device__ __forceinline__ void group_sums(const NormArgs& a, const NormPlan& p, double* s_red, double& u, double& v,
+                                           F f) {
+  const Teams t(1, a.per);
+  const int c0 = threadIdx.x % t.CL, dk = 256 / t.CL;
+  u = v = 0.0;
+  for (int64_t k = threadIdx.x / t.CL; k < p.chunks; k += dk)
+    for (int c = c0; c < a.per; c += t.CL) f(k, c, u, v);
+  u = team_sum(u, 256, s_red);
+  v = team_sum(v, 256, s_red);
+}
+
+// Block per sample and group: mean and rstd from the partial moments, to out and (nullable) stats_out.
+__global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a, NormPlan p, const float* part, float* out) {
   __shared__ double s_red[4];
   const int64_t q = a.n * p.chunks * a.channels;
+  const double total = (double)a.per * (double)a.positions;
+  auto rows = [&](int64_t k) { return (double)(min(a.positions, (k + 1) * p.rows) - k * p.rows); };
   for (int64_t b = blockIdx.x; b < a.n * a.groups; b += gridDim.x) {
-    const int64_t s = b / a.groups, c0 = b % a.groups * a.per;
-    const int64_t values = p.chunks * a.per;
-    const float* mean_p = part + s * p.chunks * a.channels + c0;
-    auto rows = [&](int64_t chunk) { return (double)(min(a.positions, (chunk + 1) * p.rows) - chunk * p.rows); };
-    auto block_sum = [&](double v) {
-      v = warp_sum(v);
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = v;
-      __syncthreads();
-      return (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]);
-    };
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < values; i += 256) {
-      const int64_t k = i / a.per, c = i % a.per;
-      sum += rows(k) * (double)mean_p[k * a.channels + c];
-    }
-    const double total = (double)a.per * (double)a.positions;
-    const double mean = block_sum(sum) / total;
-    sum = 0.0;
-    for (int64_t i = threadIdx.x; i < values; i += 256) {
-      const int64_t k = i / a.per, c = i % a.per;
+    int64_t g;
+    const int64_t s = quotient(b, a.groups, g);
+    const float* mean_p = part + s * p.chunks * a.channels + g * a.per;
+    double sum, m2, none;
+    group_sums(a, p, s_red, sum, none, [&](int64_t k, int c, double& u, double&) {
+      u += rows(k) * (double)mean_p[k * a.channels + c];
+    });
+    const double mean = sum / total;
+    group_sums(a, p, s_red, m2, none, [&](int64_t k, int c, double& u, double&) {
       const double d = (double)mean_p[k * a.channels + c] - mean;
-      sum += (double)mean_p[q + k * a.channels + c] + rows(k) * d * d;
-    }
-    const double var = block_sum(sum) / total;
+      u += (double)mean_p[q + k * a.channels + c] + rows(k) * d * d;
+    });
     if (threadIdx.x == 0) {
-      const float m = (float)mean, rstd = (float)(1.0 / sqrt(var + (double)a.eps));
-      stats[2 * b] = m;
-      stats[2 * b + 1] = rstd;
+      const float m = (float)mean, rstd = (float)(1.0 / sqrt(m2 / total + (double)a.eps));
+      out[2 * b] = m;
+      out[2 * b + 1] = rstd;
       if (a.stats_out) {
         a.stats_out[2 * b] = m;
         a.stats_out[2 * b + 1] = rstd;
@@ -604,18 +603,44 @@ __global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a, NormPlan p, 
   }
 }
 
-// What a thread of a split pass keeps of its 8 channels.
+// Block per sample and group: the means of weight dp and weight dp xh from the partial sums.
+__global__ __launch_bounds__(256) void norm_coef_kernel(NormArgs a, NormPlan p, const float* part, float* coef) {
+  __shared__ double s_red[4];
+  const int64_t q = a.n * p.chunks * a.channels;
+  const double total = (double)a.per * (double)a.positions;
+  for (int64_t b = blockIdx.x; b < a.n * a.groups; b += gridDim.x) {
+    int64_t g;
+    const int64_t s = quotient(b, a.groups, g);
+    const float* pw = part + s * p.chunks * a.channels + g * a.per;
+    double c1, c2;
+    group_sums(a, p, s_red, c1, c2, [&](int64_t k, int c, double& u, double& v) {
+      const double w = a.weight ? (double)a.weight[g * a.per + c] : 1.0;
+      u += w * (double)pw[q + k * a.channels + c];
+      v += w * (double)pw[k * a.channels + c];
+    });
+    if (threadIdx.x == 0) {
+      coef[2 * b] = (float)(c1 / total);
+      coef[2 * b + 1] = (float)(c2 / total);
+    }
+  }
+}
+
+// What a thread of a split pass keeps of its 8 channels: with d = x - mean, p = wr d + bias (wr = weight rstd).
 struct Channels {
-  float mean[8], rstd[8], w[8], b[8];
-  __device__ __forceinline__ Channels(const NormArgs& a, const float* stats, int64_t sample, int64_t c) {
+  float mean[8], wr[8], b[8];
+  __device__ __forceinline__ Channels() {}
+  // each(e, rstd, group of the sample) for what else is wanted
+  template <class Each>
+  __device__ __forceinline__ Channels(const NormArgs& a, const float* stats, int64_t sample, int64_t c, Each each) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int64_t ch = min(c + e, a.channels - 1);
-      const float* s = stats + (sample * a.groups + ch / a.per) * 2;
-      mean[e] = s[0];
-      rstd[e] = s[1];
-      w[e] = a.weight ? a.weight[ch] : 1.f;
+      const uint32_t ch = (uint32_t)min(c + e, a.channels - 1);
+      const int64_t g = sample * a.groups + ch / (uint32_t)a.per;
+      mean[e] = stats[2 * g];
+      const float rstd = stats[2 * g + 1];
+      wr[e] = (a.weight ? a.weight[ch] : 1.f) * rstd;
       b[e] = a.bias ? a.bias[ch] : 0.f;
+      each(e, rstd, g);
     }
   }
 };
@@ -627,17 +652,18 @@ __global__ __launch_bounds__(256) void norm_apply_kernel(NormArgs a, NormPlan p,
     const NormSpot at(a, p, b);
     const int64_t left = a.channels - at.c;
     if (left <= 0) continue;
-    const Channels k(a, stats, at.sample, at.c);
+    const Channels k(a, stats, at.sample, at.c, [](int, float, int64_t) {});
     const T* x = static_cast<const T*>(a.x) + at.c;
     T* y = static_cast<T*>(a.out) + at.c;
-#pragma unroll 4
-    for (int64_t r = at.r0 + at.rx; r < at.r1; r += at.lanes) {
-      float v[8];
-      load8(x + r * a.ldx, left, v);
+    constexpr int U = 4;
+    float v[U][8];
+    rows_in_groups<U>(
+        at.r0 + at.rx, at.r1, at.lanes, [&](int u, int64_t r) { load8(x + r * a.ldx, left, v[u]); },
+        [&](int u, int64_t r) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = act_value<ACT>(fmaf((v[e] - k.mean[e]) * k.rstd[e], k.w[e], k.b[e]));
-      store8(y + r * a.ldo, left, v);
-    }
+          for (int e = 0; e < 8; ++e) v[u][e] = act_value<ACT>(fmaf(v[u][e] - k.mean[e], k.wr[e], k.b[e]));
+          store8(y + r * a.ldo, left, v[u]);
+        });
   }
 }
 
@@ -653,22 +679,29 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(NormArgs a, NormPlan p, 
 #pragma unroll
     for (int e = 0; e < 8; ++e) sw[e] = sb[e] = 0.f;
     if (left > 0) {
-      const Channels k(a, a.stats, at.sample, at.c);
+      float rstd[8];
+      const Channels k(a, a.stats, at.sample, at.c, [&](int e, float r, int64_t) { rstd[e] = r; });
       const T* x = static_cast<const T*>(a.x) + at.c;
       const T* dy = static_cast<const T*>(a.dy) + at.c;
-#pragma unroll 2
-      for (int64_t r = at.r0 + at.rx; r < at.r1; r += at.lanes) {
-        float v[8], d[8];
-        load8(x + r * a.ldx, left, v);
-        load8(dy + r * a.lddy, left, d);
+      constexpr int U = 2;
+      float v[U][8], d[U][8];
+      rows_in_groups<U>(
+          at.r0 + at.rx, at.r1, at.lanes,
+          [&](int u, int64_t r) {
+            load8(x + r * a.ldx, left, v[u]);
+            load8(dy + r * a.lddy, left, d[u]);
+          },
+          [&](int u, int64_t) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float xh = (v[e] - k.mean[e]) * k.rstd[e];
-          const float dp = act_back<ACT>(d[e], fmaf(xh, k.w[e], k.b[e]));
-          sw[e] = fmaf(dp, xh, sw[e]);
-          sb[e] += dp;
-        }
-      }
+            for (int e = 0; e < 8; ++e) {
+              const float diff = v[u][e] - k.mean[e];
+              const float dp = act_back<ACT>(d[u][e], fmaf(diff, k.wr[e], k.b[e]));
+              sw[e] = fmaf(dp, diff, sw[e]);
+              sb[e] += dp;
+            }
+          });
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sw[e] *= rstd[e];
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -697,97 +730,73 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(NormArgs a, NormPlan p, 
   }
 }
 
-// Block per sample and group: the means of weight dp and weight dp xh (coef), and the sample's sums per
-// channel (sums[0 / 1][sample][channel]).
-__global__ __launch_bounds__(256) void norm_coef_kernel(NormArgs a, NormPlan p, const float* part, float* coef,
-                                                        float* sums) {
-  __shared__ double s_red[2][4];
-  const int64_t q = a.n * p.chunks * a.channels;
-  for (int64_t b = blockIdx.x; b < a.n * a.groups; b += gridDim.x) {
-    const int64_t s = b / a.groups, c0 = b % a.groups * a.per;
-    const float* pw = part + s * p.chunks * a.channels + c0;
-    double c1 = 0.0, c2 = 0.0;
-    for (int64_t c = threadIdx.x; c < a.per; c += 256) {
-      double w = 0.0, d = 0.0;
-      for (int64_t k = 0; k < p.chunks; ++k) {
-        w += (double)pw[k * a.channels + c];
-        d += (double)pw[q + k * a.channels + c];
-      }
-      sums[s * a.channels + c0 + c] = (float)w;
-      sums[(a.n + s) * a.channels + c0 + c] = (float)d;
-      const double g = a.weight ? (double)a.weight[c0 + c] : 1.0;
-      c1 += g * d;
-      c2 += g * w;
-    }
-    c1 = warp_sum(c1);
-    c2 = warp_sum(c2);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) {
-      s_red[0][threadIdx.x >> 6] = c1;
-      s_red[1][threadIdx.x >> 6] = c2;
-    }
-    __syncthreads();
-    if (threadIdx.x < 2) {
-      const double* r = s_red[threadIdx.x];
-      coef[2 * b + threadIdx.x] =
-          (float)(((r[0] + r[1]) + (r[2] + r[3])) / ((double)a.per * (double)a.positions));
-    }
-  }
-}
-
-template <class T, int ACT>
-__global__ __launch_bounds__(256) void norm_apply_back_kernel(NormArgs a, NormPlan p, const float* coef) {
-  const int64_t blocks = a.n * p.chunks * p.tiles;
-  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
-    const NormSpot at(a, p, b);
-    const int64_t left = a.channels - at.c;
-    if (left <= 0) continue;
-    const Channels k(a, a.stats, at.sample, at.c);
-    float c1[8], c2[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float* s = coef + (at.sample * a.groups + min(at.c + e, a.channels - 1) / a.per) * 2;
-      c1[e] = s[0];
-      c2[e] = s[1];
-    }
-    const T* x = static_cast<const T*>(a.x) + at.c;
-    const T* dy = static_cast<const T*>(a.dy) + at.c;
-    T* dx = static_cast<T*>(a.out) + at.c;
-#pragma unroll 2
-    for (int64_t r = at.r0 + at.rx; r < at.r1; r += at.lanes) {
-      float v[8], d[8];
-      load8(x + r * a.ldx, left, v);
-      load8(dy + r * a.lddy, left, d);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float xh = (v[e] - k.mean[e]) * k.rstd[e];
-        const float dp = act_back<ACT>(d[e], fmaf(xh, k.w[e], k.b[e])) * k.w[e];
-        v[e] = k.rstd[e] * ((dp - c1[e]) - xh * c2[e]);
-      }
-      store8(dx + r * a.ldo, left, v);
-    }
-  }
-}
-
-// out[c] = sum over k of part[k][c] in a fixed order, for both gradients (blockIdx.y): a block takes 64
-// channels, its 16 wavefronts each a sixteenth of the rows.
-__global__ __launch_bounds__(1024) void norm_gradient_kernel(const float* __restrict__ part, int64_t rows,
-                                                             int64_t channels, float* dweight, float* dbias) {
-  __shared__ float s[16][64];
-  float* out = blockIdx.y ? dbias : dweight;
+// Sums over the rows of part[0 / 1][row][channel] in a fixed order, dweight's and dbias's (nullable): block b of
+// gradient_blocks() takes 8 channels of one of them, its threads 32 rows side by side.
+__device__ __forceinline__ void gradient_block(int64_t b, const float* part, int64_t rows, int64_t channels,
+                                               float* dweight, float* dbias) {
+  __shared__ float s[256];
+  const int64_t tiles = (channels + 7) / 8, which = b / tiles;
+  float* out = which ? dbias : dweight;
   if (!out) return;                                      // the same for the whole block
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-  const float* p = part + blockIdx.y * rows * channels;
+  const int lane = threadIdx.x / 8;
+  const int64_t c = b % tiles * 8 + threadIdx.x % 8;
+  const float* p = part + which * rows * channels + c;
   float sum = 0.f;
   if (c < channels)
 #pragma unroll 8
-    for (int64_t k = wid; k < rows; k += 16) sum += p[k * channels + c];
-  s[wid][lane] = sum;
-  __syncthreads();
-  if (wid == 0 && c < channels) {
-    for (int k = 1; k < 16; ++k) sum += s[k][lane];
-    out[c] = sum;
+    for (int64_t k = lane; k < rows; k += 32) sum += p[k * channels];
+  s[threadIdx.x] = sum;
+  for (int h = 16; h > 0; h /= 2) {
+    __syncthreads();
+    if (lane < h) s[threadIdx.x] += s[threadIdx.x + 8 * h];
+  }
+  if (lane == 0 && c < channels) out[c] = s[threadIdx.x];
+}
+__global__ __launch_bounds__(256) void norm_gradient_kernel(const float* part, int64_t rows, int64_t channels,
+                                                            float* dweight, float* dbias) {
+  gradient_block(blockIdx.x, part, rows, channels, dweight, dbias);
+}
+
+// The first `extra` blocks sum dweight and dbias from norm_sums_kernel's partials beside the others.
+template <class T, int ACT>
+__global__ __launch_bounds__(256) void norm_apply_back_kernel(NormArgs a, NormPlan p, const float* coef,
+                                                              const float* part, int extra, float* dweight,
+                                                              float* dbias) {
+  if ((int)blockIdx.x < extra) {
+    gradient_block(blockIdx.x, part, a.n * p.chunks, a.channels, dweight, dbias);
+    return;
+  }
+  const int64_t blocks = a.n * p.chunks * p.tiles;
+  for (int64_t b = blockIdx.x - extra; b < blocks; b += gridDim.x - extra) {
+    const NormSpot at(a, p, b);
+    const int64_t left = a.channels - at.c;
+    if (left <= 0) continue;
+    // dx = rstd (w dp - c1 - xh c2) = wr dp - rstd c1 - (rstd^2 c2) d
+    float c1[8], c2[8];
+    const Channels k(a, a.stats, at.sample, at.c, [&](int e, float rstd, int64_t g) {
+      c1[e] = rstd * coef[2 * g];
+      c2[e] = rstd * (rstd * coef[2 * g + 1]);
+    });
+    const T* x = static_cast<const T*>(a.x) + at.c;
+    const T* dy = static_cast<const T*>(a.dy) + at.c;
+    T* dx = static_cast<T*>(a.out) + at.c;
+    constexpr int U = 2;
+    float v[U][8], d[U][8];
+    rows_in_groups<U>(
+        at.r0 + at.rx, at.r1, at.lanes,
+        [&](int u, int64_t r) {
+          load8(x + r * a.ldx, left, v[u]);
+          load8(dy + r * a.lddy, left, d[u]);
+        },
+        [&](int u, int64_t r) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float diff = v[u][e] - k.mean[e];
+            const float dp = act_back<ACT>(d[u][e], fmaf(diff, k.wr[e], k.b[e]));
+            v[u][e] = fmaf(-diff, c2[e], fmaf(dp, k.wr[e], -c1[e]));
+          }
+          store8(dx + r * a.ldo, left, v[u]);
+        });
   }
 }
 
@@ -852,9 +861,11 @@ int forward(const ot_norm* d, const ot::NormArgs& a, hipStream_t st) {
   return OT_OK;
 }
 
+int64_t gradient_blocks(int64_t channels) { return 2 * ot::ceil_div(channels, 8); }
+
 int gradients(const float* sums, int64_t rows, int64_t channels, float* dweight, float* dbias, hipStream_t st) {
-  hipLaunchKernelGGL(ot::norm_gradient_kernel, dim3((unsigned)ot::ceil_div(channels, 64), 2), dim3(1024), 0, st, sums,
-                     rows, channels, dweight, dbias);
+  hipLaunchKernelGGL(ot::norm_gradient_kernel, dim3((unsigned)gradient_blocks(channels)), dim3(256), 0, st, sums, rows,
+                     channels, dweight, dbias);
   OT_LAUNCHED("norm_gradient_kernel");
   return OT_OK;
 }
@@ -894,18 +905,18 @@ int backward(const ot_norm* d, const ot::NormArgs& a, float* dweight, float* dbi
   }
   const ot::NormPlan p = ot::plan_norm(d->sizes, a.n);
   float* coef = ws;
-  float* sums = coef + 2 * a.n * a.groups;
-  float* part = sums + 2 * a.n * a.channels;
-  const dim3 grid(grid_of(a.n * p.chunks * p.tiles));
-  hipLaunchKernelGGL((ot::norm_sums_kernel<T, ACT>), grid, dim3(256), 0, st, a, p, part);
+  float* part = coef + 2 * a.n * a.groups;
+  const unsigned blocks = grid_of(a.n * p.chunks * p.tiles);
+  hipLaunchKernelGGL((ot::norm_sums_kernel<T, ACT>), dim3(blocks), dim3(256), 0, st, a, p, part);
   OT_LAUNCHED("norm_sums_kernel");
-  hipLaunchKernelGGL(ot::norm_coef_kernel, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, coef, sums);
+  if (!a.out) return gradients(part, a.n * p.chunks, a.channels, dweight, dbias, st);
+  hipLaunchKernelGGL(ot::norm_coef_kernel, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, coef);
   OT_LAUNCHED("norm_coef_kernel");
-  if (a.out) {
-    hipLaunchKernelGGL((ot::norm_apply_back_kernel<T, ACT>), grid, dim3(256), 0, st, a, p, coef);
-    OT_LAUNCHED("norm_apply_back_kernel");
-  }
-  return want ? gradients(sums, a.n, a.channels, dweight, dbias, st) : OT_OK;
+  const int extra = want ? (int)gradient_blocks(a.channels) : 0;
+  hipLaunchKernelGGL((ot::norm_apply_back_kernel<T, ACT>), dim3(blocks + extra), dim3(256), 0, st, a, p, coef,
+                     part, extra, dweight, dbias);
+  OT_LAUNCHED("norm_apply_back_kernel");
+  return OT_OK;
 }
 
 }  // namespace

@@ -88,8 +88,7 @@ inline int64_t slab_ranges(const NormSizes& s, int64_t n) {
 }
 
 // fp32 values that calls of up to n samples need: split passes keep two sums per channel and chunk, and
-// two values per sample and group; the backward also two sums per sample and channel.  Over slabs the
-// backward keeps two sums per range and channel.
+// two values per sample and group.  Over slabs the backward keeps two sums per range and channel.
 inline int64_t norm_values(const NormSizes& s, int64_t n) {
   if (n < 1) return 0;
   if (slab_groups(s) > 0) return 2 * s.channels * std::min(n, kNormBlocks);
@@ -97,7 +96,7 @@ inline int64_t norm_values(const NormSizes& s, int64_t n) {
   const int64_t lanes = 256 / most.col_threads;
   const int64_t all = n * ceil_div(s.positions, std::max<int64_t>(16 * lanes, 64));
   const int64_t chunks = std::max(all, std::min(ceil_div(kNormBlocks, most.tiles) + n, n * ceil_div(s.positions, 2 * lanes)));
-  return 2 * (chunks * s.channels + n * s.channels + n * s.groups);
+  return 2 * (chunks * s.channels + n * s.groups);
 }
 
 }  // namespace ot

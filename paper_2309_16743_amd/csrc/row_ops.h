@@ -48,4 +48,32 @@ __device__ __forceinline__ void store8(float* p, int64_t left, const float (&v)[
   }
 }
 
+// a / b and a - a / b * b of numbers that mostly fit 32 bits (a 64-bit division takes a hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b, int64_t& rest) {
+  if (((a | b) >> 32) == 0) {
+    const uint32_t q = (uint32_t)a / (uint32_t)b;
+    rest = (uint32_t)a - q * (uint32_t)b;
+    return q;
+  }
+  const int64_t q = a / b;
+  rest = a - q * b;
+  return q;
+}
+
+// A thread's rows r, r + step, .. below end in groups of U: load(slot, row) of a whole group comes before
+// use(slot, row), since the compiler keeps loads behind stores that may alias them.
+template <int U, class Load, class Use>
+__device__ __forceinline__ void rows_in_groups(int64_t r, int64_t end, int64_t step, Load load, Use use) {
+  for (; r + (U - 1) * step < end; r += U * step) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(u, r + u * step);
+#pragma unroll
+    for (int u = 0; u < U; ++u) use(u, r + u * step);
+  }
+  for (; r < end; r += step) {
+    load(0, r);
+    use(0, r);
+  }
+}
+
 }  // namespace ot

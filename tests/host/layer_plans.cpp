@@ -79,7 +79,7 @@ static int64_t norm_used(const NormSizes& s, int64_t n) {
     return r;
   }
   const NormPlan p = plan_norm(s, n);
-  return 2 * n * s.groups + 2 * n * s.channels + 2 * n * p.chunks * s.channels;
+  return 2 * n * s.groups + 2 * n * p.chunks * s.channels;
 }
 
 static bool bounds() {
