@@ -4,6 +4,7 @@
 #include <new>
 
 #include "dense_products.h"
+#include "dense_rows.h"
 #include "layer_host.h"
 #include "layer_plan.h"
 #include "layers.h"
@@ -121,6 +122,16 @@ int run_product(ot::Product p, const ot_dense* d, const ot::ProductArgs& a, hipS
   return d->precision == OT_BF16 ? ot::run_product_bf16(p, a, st) : ot::run_product_f32(p, a, st);
 }
 
+// The layer on up to 32 rows.
+template <class T, class Y>
+int run_rows(const ot_dense* d, const ot::RowsArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)ot::ceil_div(a.N, 16)), block(256);
+  if (a.M <= 16) hipLaunchKernelGGL((ot::dense_rows_kernel<T, Y, 1>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((ot::dense_rows_kernel<T, Y, 2>), grid, block, 0, st, a);
+  OT_LAUNCHED("dense_rows_kernel");
+  return OT_OK;
+}
+
 int run_slope(const ot_dense* d, ot::SlopeArgs a, float* dbias, float* part, hipStream_t st) {
   a.plan = ot::plan_columns(a.n, a.cols);
   a.sums = dbias ? (a.plan.chunks > 1 ? part : dbias) : nullptr;
@@ -197,9 +208,15 @@ extern "C" int dense_forward(ot_dense* d, const void* x, int64_t ldx, const void
   if (pre && (rc = ot::check_rows(pre, ldp, n, d->out, e, what, "pre"))) return rc;
   if ((rc = ot::check_values(bias, 4, what, "bias"))) return rc;
   if ((rc = ot::check_device(d->device, what))) return rc;
-  const ot::ProductArgs a{x, ldx, w, ldw, n, d->out, d->in, bias, y, ldy, y_type,
-                          ot::LayerArgs{residual, ldr, pre, ldp, d->act, 1, 0}, nullptr};
-  return run_product(ot::Product::Forward, d, a, static_cast<hipStream_t>(stream));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const ot::LayerArgs ly{residual, ldr, pre, ldp, d->act, 1, 0};
+  if (ot::few_rows(e == 2, n, d->out, d->in)) {
+    const ot::RowsArgs a{x, ldx, w, ldw, n, d->out, d->in, bias, y, ldy, ly};
+    if (e == 2) return ey == 2 ? run_rows<uint16_t, uint16_t>(d, a, st) : run_rows<uint16_t, float>(d, a, st);
+    return ey == 2 ? run_rows<float, uint16_t>(d, a, st) : run_rows<float, float>(d, a, st);
+  }
+  const ot::ProductArgs a{x, ldx, w, ldw, n, d->out, d->in, bias, y, ldy, y_type, ly, nullptr};
+  return run_product(ot::Product::Forward, d, a, st);
 }
 
 extern "C" int dense_backward(ot_dense* d, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n,

@@ -95,6 +95,14 @@ inline DensePlan plan_dense(bool bf16, Product product, int64_t M, int64_t N, in
 // The splits that are not empty, in whole k tiles.
 inline AdaptPlan split_dense(const DensePlan& d, int64_t K) { return split_plan(d.tile, K, d.want); }
 
+// Whether the layer runs on dense_rows.h: few rows, and so little in all that the loads of x do not count
+// (us there, and tiled: bf16 32 rows of 2048 x 2048 9, 17, of 2048 x 16384 24, 16; 8 rows of 2048 x 16384 14.7, 15,
+// of 2048 x 100000 92, 97; fp32 8, 16 rows of 1024 x 200000 175, 200 and 212, 204; 32 of 256 x 32768 14.8, 16.7).
+inline bool few_rows(bool bf16, int64_t M, int64_t N, int64_t K) {
+  if (M > 32) return false;
+  return M <= (bf16 ? 1 : 8) || M * N * K <= (1LL << (bf16 ? 28 : 29));
+}
+
 // Sums over the rows of n x cols values: a thread holds 8 columns, a block of 256 threads
 // col_threads x 8 columns and `rows` rows; `chunks` partial sums per column (1: the sum itself).
 struct ColumnPlan {

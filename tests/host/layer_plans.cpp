@@ -25,7 +25,12 @@ static void dense_kernels(int64_t n, int64_t in, int64_t out, std::set<std::stri
         snprintf(b, sizeof b, "%s bf16=%d tile=%d split=%d", what, bf, a.tile, a.splits > 1);
         s.insert(b);
       };
-      add("forward", Product::Forward, n, out, in, 1);
+      if (few_rows(bf, n, out, in)) {
+        snprintf(b, sizeof b, "forward bf16=%d rows=%d", bf, n > 16);
+        s.insert(b);
+      } else {
+        add("forward", Product::Forward, n, out, in, 1);
+      }
       add("dx", Product::InputGrad, n, in, out, dx_planes(d));
       add("dw", Product::WeightGrad, out, in, n, std::max(1, planes));
       snprintf(b, sizeof b, "columns chunks=%d", plan_columns(n, out).chunks > 1);
@@ -127,7 +132,7 @@ int main(int argc, char** argv) {
     return ok ? 0 : 1;
   }
   if (argc == 2 && !strcmp(argv[1], "dense")) {
-    const int64_t sizes[] = {1, 6, 30, 64, 65, 100, 128, 129, 200, 300, 512, 600, 1024, 2048, 5000, 10000, 40000, 100000, 1000000};
+    const int64_t sizes[] = {1, 6, 20, 30, 64, 65, 100, 128, 129, 200, 300, 512, 600, 1024, 2048, 5000, 10000, 40000, 100000, 1000000};
     for (int64_t n : sizes)
       for (int64_t in : sizes)
         for (int64_t out : sizes) dense_kernels(n, in, out, s);
