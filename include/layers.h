@@ -59,7 +59,7 @@ enum ot_activation { OT_ACT_NONE = 0, OT_ACT_RELU = 1, OT_ACT_SILU = 2, OT_ACT_G
  * workspaces are first sized for, in [0, 2^26] (0: a layer that only serves; a
  * forward needs none).  A backward's workspace holds dz where there is an activation
  * (fp32, relu in bf16: as large as dy; silu and gelu in bf16: three times) and at most
- * 0.14 GB of partial sums.  Errors: OT_E_INVAL, OT_E_NOMEM, OT_E_HIP. */
+ * 0.3 GB of partial sums.  Errors: OT_E_INVAL, OT_E_NOMEM, OT_E_HIP. */
 int dense_create(ot_dense** out, int64_t in, int64_t out_dim, int32_t precision, int32_t activation,
                  int64_t max_rows);
 

@@ -21,7 +21,8 @@ struct SlopeArgs {
   void* dz;                 // rows of lddz values, planes plane_stride elements apart
   int64_t lddz, plane_stride;
   int64_t n, cols;
-  float* sums;              // [chunk][cols] (nullable)
+  float* sums;              // [chunk] rows of sums_ld values (nullable)
+  int64_t sums_ld;
   ColumnPlan plan;
 };
 
@@ -72,25 +73,57 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
   }
   if (rx == 0)
     for (int e = 0; e < 8; ++e)
-      if (c + e < a.cols) a.sums[blockIdx.y * a.cols + c + e] = s[threadIdx.x][e];
+      if (c + e < a.cols) a.sums[blockIdx.y * a.sums_ld + c + e] = s[threadIdx.x][e];
 }
 
-// Sums of the chunks' partials in a fixed order: a block takes 64 columns, its 16 wavefronts each a
-// sixteenth of the chunks.
-__global__ __launch_bounds__(1024) void column_join_kernel(const float* __restrict__ part, int64_t chunks, int64_t cols,
-                                                           float* __restrict__ out) {
-  __shared__ float s[16][64];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-  float sum = 0.f;
-  if (c < cols)
-#pragma unroll 8
-    for (int64_t k = wid; k < chunks; k += 16) sum += part[k * cols + c];
-  s[wid][lane] = sum;
-  __syncthreads();
-  if (wid == 0 && c < cols) {
-    for (int k = 1; k < 16; ++k) sum += s[k][lane];
-    out[c] = sum;
+// All the sums that a backward leaves: of the split products, and of the chunks' column sums.  A thread sums four
+// neighbouring values; where the splits are many, `lanes` threads share them.
+struct JoinJobs {
+  JoinJob job[3];
+  int64_t blocks[3];
+};
+__global__ __launch_bounds__(256) void dense_join_kernel(JoinJobs jobs) {
+  __shared__ f32x4 s[256];
+  int64_t b = blockIdx.x;
+  int k = 0;
+  while (b >= jobs.blocks[k]) b -= jobs.blocks[k++];
+  const JoinJob& j = jobs.job[k];
+  const int per = 256 / j.lanes, lane = threadIdx.x / per;
+  const int64_t groups = (j.N + 3) / 4, i = b * per + threadIdx.x % per;
+  const bool in = i < j.M * groups;
+  int64_t col;
+  const int64_t m = quotient(in ? i : 0, groups, col), n = 4 * col;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (in) {
+    const float* p = j.part + m * j.ldp + n;
+    int q = lane;
+    for (; q + 7 * j.lanes < j.splits; q += 8 * j.lanes) {   // eight loads in flight, added in order
+      f32x4 t[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) t[u] = *reinterpret_cast<const f32x4*>(p + (q + u * j.lanes) * j.stride);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v += t[u];
+    }
+    for (; q < j.splits; q += j.lanes) v += *reinterpret_cast<const f32x4*>(p + q * j.stride);
+  }
+  if (j.lanes > 1) {                                     // the same for the whole block
+    s[threadIdx.x] = v;
+    for (int h = j.lanes / 2; h > 0; h /= 2) {
+      __syncthreads();
+      if (lane < h) s[threadIdx.x] += s[threadIdx.x + h * per];
+    }
+    v = s[threadIdx.x];
+  }
+  if (!in || lane > 0) return;
+  const int cnt = (int)min((int64_t)4, j.N - n);
+  if (j.c_type == OT_BF16) {
+    uint16_t* out = static_cast<uint16_t*>(j.C) + m * j.ldc + n;
+    for (int c = 0; c < cnt; ++c) out[c] = lr_bf16(v[c]);
+  } else {
+    float* out = static_cast<float*>(j.C) + m * j.ldc + n;
+    if (cnt == 4 && reinterpret_cast<uintptr_t>(out) % 16 == 0) *reinterpret_cast<f32x4*>(out) = v;
+    else
+      for (int c = 0; c < cnt; ++c) out[c] = v[c];
   }
 }
 
@@ -118,8 +151,8 @@ namespace {
 
 constexpr int64_t kMost = 1LL << 26, kMostValues = 1LL << 36;
 
-int run_product(ot::Product p, const ot_dense* d, const ot::ProductArgs& a, hipStream_t st) {
-  return d->precision == OT_BF16 ? ot::run_product_bf16(p, a, st) : ot::run_product_f32(p, a, st);
+int run_product(ot::Product p, const ot_dense* d, const ot::ProductArgs& a, ot::JoinJob* join, hipStream_t st) {
+  return d->precision == OT_BF16 ? ot::run_product_bf16(p, a, join, st) : ot::run_product_f32(p, a, join, st);
 }
 
 // The layer on up to 32 rows.
@@ -132,9 +165,12 @@ int run_rows(const ot_dense* d, const ot::RowsArgs& a, hipStream_t st) {
   return OT_OK;
 }
 
-int run_slope(const ot_dense* d, ot::SlopeArgs a, float* dbias, float* part, hipStream_t st) {
+// dz and the column sums; where those are partial, their join is left to the caller.
+int run_slope(const ot_dense* d, ot::SlopeArgs a, float* dbias, float* part, ot::JoinJob* join, hipStream_t st) {
   a.plan = ot::plan_columns(a.n, a.cols);
-  a.sums = dbias ? (a.plan.chunks > 1 ? part : dbias) : nullptr;
+  const bool split = a.plan.chunks > 1;
+  a.sums = dbias && split ? part : dbias;
+  a.sums_ld = ot::round_up(a.cols, 4);
   const dim3 grid((unsigned)a.plan.blocks_x, (unsigned)a.plan.chunks), block(256);
   ot::with_act(d->act, [&](auto act) {
     constexpr int A = decltype(act)::value;
@@ -143,11 +179,22 @@ int run_slope(const ot_dense* d, ot::SlopeArgs a, float* dbias, float* part, hip
     else hipLaunchKernelGGL((ot::slope_kernel<uint16_t, TERMS, A>), grid, block, 0, st, a);
   });
   OT_LAUNCHED("slope_kernel");
-  if (dbias && a.plan.chunks > 1) {
-    hipLaunchKernelGGL(ot::column_join_kernel, dim3((unsigned)ot::ceil_div(a.cols, 64)), dim3(1024), 0, st, part,
-                       a.plan.chunks, a.cols, dbias);
-    OT_LAUNCHED("column_join_kernel");
+  if (dbias && split)
+    *join = ot::JoinJob{part, a.sums_ld, a.sums_ld, (int32_t)a.plan.chunks, 16, 1, a.cols, dbias, a.cols, OT_FP32};
+  return OT_OK;
+}
+
+int run_joins(const ot::JoinJob (&job)[3], hipStream_t st) {
+  ot::JoinJobs jobs{};
+  int64_t blocks = 0;
+  for (int k = 0; k < 3; ++k) {
+    jobs.job[k] = job[k];
+    if (job[k].splits) jobs.blocks[k] = ot::ceil_div(job[k].M * ot::ceil_div(job[k].N, 4), 256 / job[k].lanes);
+    blocks += jobs.blocks[k];
   }
+  if (blocks == 0) return OT_OK;
+  hipLaunchKernelGGL(ot::dense_join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, jobs);
+  OT_LAUNCHED("dense_join_kernel");
   return OT_OK;
 }
 
@@ -216,7 +263,7 @@ extern "C" int dense_forward(ot_dense* d, const void* x, int64_t ldx, const void
     return ey == 2 ? run_rows<float, uint16_t>(d, a, st) : run_rows<float, float>(d, a, st);
   }
   const ot::ProductArgs a{x, ldx, w, ldw, n, d->out, d->in, bias, y, ldy, y_type, ly, nullptr};
-  return run_product(ot::Product::Forward, d, a, st);
+  return run_product(ot::Product::Forward, d, a, nullptr, st);
 }
 
 extern "C" int dense_backward(ot_dense* d, const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t n,
@@ -251,26 +298,29 @@ extern "C" int dense_backward(ot_dense* d, const void* x, int64_t ldx, const voi
   if ((rc = d->ws.begin(n, st, what, [&](int64_t rows) { return d->bytes(rows); }))) return rc;
   const int64_t ldz = sz.planes ? ot::dz_ld(sz) : lddy;
   void* dz = sz.planes ? d->ws.p : const_cast<void*>(dy);
-  float* part = reinterpret_cast<float*>(d->ws.p + ot::dz_bytes(sz, n));
+  float* const dw_part = reinterpret_cast<float*>(d->ws.p + ot::dz_bytes(sz, n));
+  float* const dx_part = dw_part + ot::round_up(ot::dw_values(sz, n), 4);
+  float* const db_part = dx_part + ot::round_up(ot::dx_values(sz, n), 4);
+  ot::JoinJob join[3] = {};                              // dw, dx, dbias
   if (sz.planes || dbias) {
-    const ot::SlopeArgs s{dy, lddy, pre, ldp, dz, ldz, n * ldz, n, d->out, nullptr, {}};
-    if ((rc = run_slope(d, s, dbias, part, st))) return rc;
+    const ot::SlopeArgs s{dy, lddy, pre, ldp, dz, ldz, n * ldz, n, d->out, nullptr, 0, {}};
+    if ((rc = run_slope(d, s, dbias, db_part, &join[2], st))) return rc;
   }
   ot::LayerArgs ly{};
   ly.planes = std::max(1, sz.planes);
   ly.plane_stride = n * ldz;
   if (dw) {
-    const ot::ProductArgs a{dz, ldz, x, ldx, d->out, d->in, n, nullptr, dw, lddw, OT_FP32, ly, part};
-    if ((rc = run_product(ot::Product::WeightGrad, d, a, st))) return rc;
+    const ot::ProductArgs a{dz, ldz, x, ldx, d->out, d->in, n, nullptr, dw, lddw, OT_FP32, ly, dw_part};
+    if ((rc = run_product(ot::Product::WeightGrad, d, a, &join[0], st))) return rc;
   }
   if (dx) {
     // a bf16 dx takes the first two terms: they leave 2^-18 of dz, as much as rounding sums of thousands of
     // products to fp32 does, of a result that keeps 2^-9 (1024 x 2048 x 2048: 28 us, 42 with three)
     ly.planes = ot::dx_planes(sz);
-    const ot::ProductArgs a{dz, ldz, w, ldw, n, d->in, d->out, nullptr, dx, lddx, d->precision, ly, part};
-    if ((rc = run_product(ot::Product::InputGrad, d, a, st))) return rc;
+    const ot::ProductArgs a{dz, ldz, w, ldw, n, d->in, d->out, nullptr, dx, lddx, d->precision, ly, dx_part};
+    if ((rc = run_product(ot::Product::InputGrad, d, a, &join[1], st))) return rc;
   }
-  return OT_OK;
+  return run_joins(join, st);
 } catch (const std::bad_alloc&) {
   return ot::set_error(OT_E_NOMEM, "dense_backward: out of host memory");
 }

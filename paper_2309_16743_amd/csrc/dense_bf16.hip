@@ -37,7 +37,7 @@ hipError_t launch(int tile, const GemmBArgs& g, int64_t splits, hipStream_t st) 
 
 }  // namespace
 
-int run_product_bf16(Product p, const ProductArgs& a, hipStream_t st) {
+int run_product_bf16(Product p, const ProductArgs& a, JoinJob* join, hipStream_t st) {
   const AdaptPlan plan = split_dense(plan_dense(true, p, a.M, a.N, a.K, a.ly.planes), a.K);
   GemmBArgs g{};
   g.A = static_cast<const uint16_t*>(a.A);
@@ -70,9 +70,8 @@ int run_product_bf16(Product p, const ProductArgs& a, hipStream_t st) {
                : launch<Product::WeightGrad, EpiB::LayerF32>(plan.tile, g, 1, st);
   if (rc != hipSuccess)
     return set_error(OT_E_HIP, "launch of the dense product failed: %s", hipGetErrorString(rc));
-  if (!split) return OT_OK;
-  return p == Product::InputGrad ? join_splits<uint16_t>(a, plan.splits, g.split_stride, g.ldc, st)
-                                 : join_splits<float>(a, plan.splits, g.split_stride, g.ldc, st);
+  if (split) *join = split_join(a, plan.splits, g.split_stride, g.ldc);
+  return OT_OK;
 }
 
 }  // namespace ot

@@ -32,7 +32,7 @@ hipError_t launch(int tile, const GemmArgs& g, int64_t splits, hipStream_t st) {
 
 }  // namespace
 
-int run_product_f32(Product p, const ProductArgs& a, hipStream_t st) {
+int run_product_f32(Product p, const ProductArgs& a, JoinJob* join, hipStream_t st) {
   const AdaptPlan plan = split_dense(plan_dense(false, p, a.M, a.N, a.K, 1), a.K);
   GemmArgs g{};
   g.A = static_cast<const float*>(a.A);
@@ -65,7 +65,8 @@ int run_product_f32(Product p, const ProductArgs& a, hipStream_t st) {
                : launch<Product::WeightGrad, Epi::Store>(plan.tile, g, 1, st);
   if (rc != hipSuccess)
     return set_error(OT_E_HIP, "launch of the dense product failed: %s", hipGetErrorString(rc));
-  return split ? join_splits<float>(a, plan.splits, g.split_stride, g.ldc, st) : OT_OK;
+  if (split) *join = split_join(a, plan.splits, g.split_stride, g.ldc);
+  return OT_OK;
 }
 
 }  // namespace ot

@@ -118,14 +118,14 @@ inline ColumnPlan plan_columns(int64_t n, int64_t cols) {
   p.blocks_x = ceil_div(groups, p.col_threads);
   const int64_t lanes = 256 / p.col_threads;             // rows side by side
   const int64_t most = std::max<int64_t>(1, ceil_div(n, 4 * lanes));
-  p.chunks = std::max<int64_t>(1, std::min(most, kColumnBlocks / p.blocks_x));
+  p.chunks = p.blocks_x >= 256 ? 1 : std::max<int64_t>(1, std::min(most, kColumnBlocks / p.blocks_x));
   p.rows = ceil_div(ceil_div(std::max<int64_t>(n, 1), p.chunks), lanes) * lanes;
   p.chunks = std::max<int64_t>(1, ceil_div(n, p.rows));
   return p;
 }
 inline int64_t column_values(int64_t n, int64_t cols) {
   const int64_t c = plan_columns(n, cols).chunks;
-  return c > 1 ? c * cols : 0;
+  return c > 1 ? c * round_up(cols, 4) : 0;
 }
 
 // Sizes of a dense layer and what its backward keeps.
@@ -150,17 +150,18 @@ inline int64_t dx_values(const DenseSizes& d, int64_t n) {
 inline int64_t dw_values(const DenseSizes& d, int64_t n) {
   return product_values(d.bf16, Product::WeightGrad, d.out, d.in, n, std::max(1, d.planes));
 }
-// Partial sums that calls of up to n rows need (the products run one after the other and share them).
+// Partial sums that calls of up to n rows need: of the weight gradient, of the input gradient and of the columns.
 inline int64_t dense_values(const DenseSizes& d, int64_t n) {
   if (n < 1) return 0;
-  // column sums: chunks * blocks_x <= kColumnBlocks
-  int64_t most = std::min(kColumnBlocks * 256 * 8, ceil_div(n, 4) * d.out);
+  // columns: chunks * blocks_x <= kColumnBlocks, and a chunk has at least 4 rows
+  const int64_t db = std::min(kColumnBlocks * 256 * 8, ceil_div(n, 4) * round_up(d.out, 4));
   // the weight gradient: the tile changes at kLongRows only, and the splits asked for grow with the rows
-  most = std::max(most, std::max(dw_values(d, n), dw_values(d, std::min(n, kLongRows - 1))));
+  const int64_t dw = std::max(dw_values(d, n), dw_values(d, std::min(n, kLongRows - 1)));
   // the input gradient: a plan depends on the rows only through whole groups of 32, and past 65536 of them
   // there are so many tiles that nothing is split
-  for (int64_t m = 32; m < std::min<int64_t>(n, 65536) + 32; m += 32) most = std::max(most, dx_values(d, m));
-  return most;
+  int64_t dx = 0;
+  for (int64_t m = 32; m < std::min<int64_t>(n, 65536) + 32; m += 32) dx = std::max(dx, dx_values(d, m));
+  return round_up(dw, 4) + round_up(dx, 4) + db;
 }
 
 }  // namespace ot
