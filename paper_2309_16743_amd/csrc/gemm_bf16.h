@@ -1006,6 +1006,25 @@ __device__ __forceinline__ void layer_tail(const GemmBArgs& g, Acc (&acc)[FM][FN
   }
 }
 
+// Layer*: a weight gradient straight from the accumulators, rows mw.. and columns nw.. of a wavefront: a store
+// writes 128 bytes of each of two rows, and no wavefront waits for another.
+template <int FM, int FN, class Acc>
+__device__ __forceinline__ void layer_store(const GemmBArgs& g, const Acc (&acc)[FM][FN], int64_t mw, int64_t nw,
+                                            int lane) {
+  float* const C = reinterpret_cast<float*>(g.C);
+  const int64_t m = mw + 4 * (lane / 32), n = nw + lane % 32;
+#pragma unroll
+  for (int f = 0; f < FM; ++f)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int64_t row = m + 32 * f + 8 * (r / 4) + r % 4;
+      if (row >= g.M) continue;
+#pragma unroll
+      for (int h = 0; h < FN; ++h)
+        if (n + 32 * h < g.N) __builtin_nontemporal_store(acc[f][h][r], C + row * g.ldc + n + 32 * h);
+    }
+}
+
 // Adapt*: the low-rank products of the tile's rows added to the sums (acc: 32 x 32 fragments of
 // wavefront rows wr.. and columns wc.. of the tile).  The block brings the 16-rank slices of all
 // adapters that its rows name into LDS (as many as fit into `bytes` at once: one
@@ -1324,6 +1343,10 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
   bool odd = false;
   if constexpr (is_layer(EPI))
     layer_tail<FM, FN, LA, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nkp * BK, kend, lane);
+  if constexpr (EPI == EpiB::LayerF32 && LA == LayB::MNMajor) {
+    layer_store<FM, FN>(g, acc, m0 + WM * wm, n0 + WN * wn, lane);
+    return;
+  }
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
     if (split == 0)
@@ -1528,6 +1551,10 @@ __global__ __launch_bounds__(512, 1) void gemm_bf16_pp_kernel(GemmBArgs g) {
   bool odd = false;
   if constexpr (is_layer(EPI))
     layer_tail<FM, FN, LA, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nkp * BK, kend, lane);
+  if constexpr (EPI == EpiB::LayerF32 && LA == LayB::MNMajor) {
+    layer_store<FM, FN>(g, acc, m0 + WM * wm, n0 + WN * wn, lane);
+    return;
+  }
   if constexpr (is_adapt(EPI)) {
     adapt_tail<FM, FN, LB>(g, acc, m0 + WM * wm, n0 + WN * wn, kbeg + (int64_t)nk * BK, kend, lane);
     if (split == 0)
