@@ -982,7 +982,9 @@ extern "C" int norm_forward(ot_norm* d, const void* x, int64_t ldx, const float*
   if ((rc = ot::check_values(stats, 4, what, "stats"))) return rc;
   if ((rc = ot::check_device(d->device, what))) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if ((rc = d->ws.begin(n, st, what, [&](int64_t k) { return d->bytes(k); }))) return rc;
+  // only split passes keep something between launches
+  if (ot::slab_groups(d->sizes) == 0 && (rc = d->ws.begin(n, st, what, [&](int64_t k) { return d->bytes(k); })))
+    return rc;
   ot::NormArgs a = args_of(d, n);
   a.x = x;
   a.ldx = ldx;
