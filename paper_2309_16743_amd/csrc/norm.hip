@@ -1,9 +1,9 @@
 // Group norm with an activation over channels-last data (include/layers.h).
 //
-// Two forms.  Where a sample's group fits into LDS (8192 values), a block keeps some of a
-// sample's groups there: mean, then the squares of the differences from it, then the results, and
-// x is read once.  Longer groups take three launches: partial moments per chunk of
-// positions and channel, their join per sample and group, the results (x is read twice,
+// Three forms (norm_plan.h).  Up to 4 positions, groups of whole vectors of 8 channels: in registers of a team of
+// lanes.  Few positions otherwise: a block keeps some of a sample's groups in LDS.  Both read x once: mean, the
+// squares of the differences from it, the results.  Many positions, or longer groups, take three launches: partial
+// moments per chunk of positions and channel, their join per sample and group, the results (x is read twice,
 // the second time from the Infinity Cache where it fits).  No atomics: every sum has a fixed order.
 #include <cmath>
 #include <new>
@@ -298,9 +298,12 @@ __device__ __forceinline__ void slab_store(T* p, bool aligned, int left, const f
 
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void norm_slab_kernel(NormArgs a, int gb, int64_t parts) {
-  __shared__ float tile[kSlab];
-  __shared__ float s_mean[kSlabGroups], s_rstd[kSlabGroups], s_red[4];
+  extern __shared__ float s_dyn[];                         // slab_values()
+  __shared__ float s_red[4];
   const int P = (int)a.positions;
+  float* const tile = s_dyn;
+  float* const s_mean = tile + gb * a.per * P;
+  float* const s_rstd = s_mean + gb;
   for (int64_t b = blockIdx.x; b < a.n * parts; b += gridDim.x) {
     const int64_t s = b / parts, g0 = b % parts * gb;
     const int groups = (int)min((int64_t)gb, a.groups - g0), width = groups * a.per;
@@ -374,10 +377,15 @@ __global__ __launch_bounds__(256) void norm_slab_kernel(NormArgs a, int gb, int6
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void norm_slab_back_kernel(NormArgs a, int gb, int64_t parts, int64_t ranges,
                                                              float* sums) {
-  __shared__ float t_dp[kSlab], t_xh[kSlab];
-  __shared__ float s_w[kSlab], s_b[kSlab];                 // sums of the range so far
-  __shared__ float s_c1[kSlabGroups], s_c2[kSlabGroups], s_red[4];
-  const int P = (int)a.positions;
+  extern __shared__ float s_dyn[];                         // slab_values()
+  __shared__ float s_red[4];
+  const int P = (int)a.positions, full = gb * a.per;
+  float* const t_dp = s_dyn;
+  float* const t_xh = t_dp + full * P;
+  float* const s_w = t_xh + full * P;                      // sums of the range so far
+  float* const s_b = s_w + full;
+  float* const s_c1 = s_b + full;
+  float* const s_c2 = s_c1 + gb;
   const int64_t part = blockIdx.x % parts, range = blockIdx.x / parts;
   const int64_t g0 = part * gb, c0 = g0 * a.per;
   const int groups = (int)min((int64_t)gb, a.groups - g0), width = groups * a.per;
@@ -559,39 +567,45 @@ __global__ __launch_bounds__(256) void norm_moments_kernel(NormArgs a, NormPlan 
   }
 }
 
-// Sums over a group's partial values in 64 bits by a whole block: f(chunk, channel, u, v) adds to u and v.
-template <class F>
-__device__ __forceinline__ void group_sums(const NormArgs& a, const NormPlan& p, double* s_red, double& u, double& v,
-                                           F f) {
-  const Teams t(1, a.per);
-  const int c0 = threadIdx.x % t.CL, dk = 256 / t.CL;
+// Sums over a group's partial values in 64 bits by a team of S threads: f(chunk, channel, u, v) adds to u and v.  All
+// threads of the block call it together.
+template <int S, class F>
+__device__ __forceinline__ void group_sums(const NormArgs& a, const NormPlan& p, bool in, double* s_red, double& u,
+                                           double& v, F f) {
+  int CL = 1;                                            // threads side by side along the channels
+  while (CL < S && CL < a.per) CL <<= 1;
+  const int me = threadIdx.x % S, dk = S / CL;
   u = v = 0.0;
-  for (int64_t k = threadIdx.x / t.CL; k < p.chunks; k += dk)
-    for (int c = c0; c < a.per; c += t.CL) f(k, c, u, v);
-  u = team_sum(u, 256, s_red);
-  v = team_sum(v, 256, s_red);
+  if (in)
+    for (int64_t k = me / CL; k < p.chunks; k += dk)
+      for (int c = me % CL; c < a.per; c += CL) f(k, c, u, v);
+  u = team_sum(u, S, s_red);
+  v = team_sum(v, S, s_red);
 }
 
-// Block per sample and group: mean and rstd from the partial moments, to out and (nullable) stats_out.
+// Team per sample and group: mean and rstd from the partial moments, to out and (nullable) stats_out.
+template <int S>
 __global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a, NormPlan p, const float* part, float* out) {
   __shared__ double s_red[4];
-  const int64_t q = a.n * p.chunks * a.channels;
+  const int64_t q = a.n * p.chunks * a.channels, all = a.n * a.groups;
   const double total = (double)a.per * (double)a.positions;
   auto rows = [&](int64_t k) { return (double)(min(a.positions, (k + 1) * p.rows) - k * p.rows); };
-  for (int64_t b = blockIdx.x; b < a.n * a.groups; b += gridDim.x) {
+  for (int64_t b0 = (int64_t)blockIdx.x * (256 / S); b0 < all; b0 += (int64_t)gridDim.x * (256 / S)) {
+    const int64_t b = b0 + threadIdx.x / S;
+    const bool in = b < all;
     int64_t g;
-    const int64_t s = quotient(b, a.groups, g);
+    const int64_t s = quotient(in ? b : 0, a.groups, g);
     const float* mean_p = part + s * p.chunks * a.channels + g * a.per;
     double sum, m2, none;
-    group_sums(a, p, s_red, sum, none, [&](int64_t k, int c, double& u, double&) {
+    group_sums<S>(a, p, in, s_red, sum, none, [&](int64_t k, int c, double& u, double&) {
       u += rows(k) * (double)mean_p[k * a.channels + c];
     });
     const double mean = sum / total;
-    group_sums(a, p, s_red, m2, none, [&](int64_t k, int c, double& u, double&) {
+    group_sums<S>(a, p, in, s_red, m2, none, [&](int64_t k, int c, double& u, double&) {
       const double d = (double)mean_p[k * a.channels + c] - mean;
       u += (double)mean_p[q + k * a.channels + c] + rows(k) * d * d;
     });
-    if (threadIdx.x == 0) {
+    if (in && threadIdx.x % S == 0) {
       const float m = (float)mean, rstd = (float)(1.0 / sqrt(m2 / total + (double)a.eps));
       out[2 * b] = m;
       out[2 * b + 1] = rstd;
@@ -603,22 +617,25 @@ __global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a, NormPlan p, 
   }
 }
 
-// Block per sample and group: the means of weight dp and weight dp xh from the partial sums.
+// Team per sample and group: the means of weight dp and weight dp xh from the partial sums.
+template <int S>
 __global__ __launch_bounds__(256) void norm_coef_kernel(NormArgs a, NormPlan p, const float* part, float* coef) {
   __shared__ double s_red[4];
-  const int64_t q = a.n * p.chunks * a.channels;
+  const int64_t q = a.n * p.chunks * a.channels, all = a.n * a.groups;
   const double total = (double)a.per * (double)a.positions;
-  for (int64_t b = blockIdx.x; b < a.n * a.groups; b += gridDim.x) {
+  for (int64_t b0 = (int64_t)blockIdx.x * (256 / S); b0 < all; b0 += (int64_t)gridDim.x * (256 / S)) {
+    const int64_t b = b0 + threadIdx.x / S;
+    const bool in = b < all;
     int64_t g;
-    const int64_t s = quotient(b, a.groups, g);
+    const int64_t s = quotient(in ? b : 0, a.groups, g);
     const float* pw = part + s * p.chunks * a.channels + g * a.per;
     double c1, c2;
-    group_sums(a, p, s_red, c1, c2, [&](int64_t k, int c, double& u, double& v) {
+    group_sums<S>(a, p, in, s_red, c1, c2, [&](int64_t k, int c, double& u, double& v) {
       const double w = a.weight ? (double)a.weight[g * a.per + c] : 1.0;
       u += w * (double)pw[q + k * a.channels + c];
       v += w * (double)pw[k * a.channels + c];
     });
-    if (threadIdx.x == 0) {
+    if (in && threadIdx.x % S == 0) {
       coef[2 * b] = (float)(c1 / total);
       coef[2 * b + 1] = (float)(c2 / total);
     }
@@ -844,7 +861,8 @@ int forward(const ot_norm* d, const ot::NormArgs& a, hipStream_t st) {
   const int gb = ot::slab_groups(d->sizes);
   if (gb > 0) {
     const int64_t parts = ot::ceil_div(a.groups, gb);
-    hipLaunchKernelGGL((ot::norm_slab_kernel<T, ACT>), dim3(grid_of(a.n * parts)), dim3(256), 0, st, a, gb, parts);
+    hipLaunchKernelGGL((ot::norm_slab_kernel<T, ACT>), dim3(grid_of(a.n * parts)), dim3(256),
+                       (unsigned)(4 * ot::slab_values(d->sizes, false)), st, a, gb, parts);
     OT_LAUNCHED("norm_slab_kernel");
     return OT_OK;
   }
@@ -854,7 +872,11 @@ int forward(const ot_norm* d, const ot::NormArgs& a, hipStream_t st) {
   const dim3 grid(grid_of(a.n * p.chunks * p.tiles));
   hipLaunchKernelGGL(ot::norm_moments_kernel<T>, grid, dim3(256), 0, st, a, p, part);
   OT_LAUNCHED("norm_moments_kernel");
-  hipLaunchKernelGGL(ot::norm_join_kernel, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, stats);
+  if (ot::long_join(d->sizes, p))
+    hipLaunchKernelGGL(ot::norm_join_kernel<256>, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, stats);
+  else
+    hipLaunchKernelGGL(ot::norm_join_kernel<64>, dim3(grid_of(ot::ceil_div(a.n * a.groups, 4))), dim3(256), 0, st, a, p,
+                       part, stats);
   OT_LAUNCHED("norm_join_kernel");
   hipLaunchKernelGGL((ot::norm_apply_kernel<T, ACT>), grid, dim3(256), 0, st, a, p, stats);
   OT_LAUNCHED("norm_apply_kernel");
@@ -898,8 +920,8 @@ int backward(const ot_norm* d, const ot::NormArgs& a, float* dweight, float* dbi
   }
   if (gb > 0) {
     const int64_t parts = ot::ceil_div(a.groups, gb), ranges = ot::slab_ranges(d->sizes, a.n);
-    hipLaunchKernelGGL((ot::norm_slab_back_kernel<T, ACT>), dim3((unsigned)(parts * ranges)), dim3(256), 0, st, a, gb, parts,
-                       ranges, want ? ws : nullptr);
+    hipLaunchKernelGGL((ot::norm_slab_back_kernel<T, ACT>), dim3((unsigned)(parts * ranges)), dim3(256),
+                       (unsigned)(4 * ot::slab_values(d->sizes, true)), st, a, gb, parts, ranges, want ? ws : nullptr);
     OT_LAUNCHED("norm_slab_back_kernel");
     return want ? gradients(ws, ranges, a.channels, dweight, dbias, st) : OT_OK;
   }
@@ -910,7 +932,11 @@ int backward(const ot_norm* d, const ot::NormArgs& a, float* dweight, float* dbi
   hipLaunchKernelGGL((ot::norm_sums_kernel<T, ACT>), dim3(blocks), dim3(256), 0, st, a, p, part);
   OT_LAUNCHED("norm_sums_kernel");
   if (!a.out) return gradients(part, a.n * p.chunks, a.channels, dweight, dbias, st);
-  hipLaunchKernelGGL(ot::norm_coef_kernel, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, coef);
+  if (ot::long_join(d->sizes, p))
+    hipLaunchKernelGGL(ot::norm_coef_kernel<256>, dim3(grid_of(a.n * a.groups)), dim3(256), 0, st, a, p, part, coef);
+  else
+    hipLaunchKernelGGL(ot::norm_coef_kernel<64>, dim3(grid_of(ot::ceil_div(a.n * a.groups, 4))), dim3(256), 0, st, a, p,
+                       part, coef);
   OT_LAUNCHED("norm_coef_kernel");
   const int extra = want ? (int)gradient_blocks(a.channels) : 0;
   hipLaunchKernelGGL((ot::norm_apply_back_kernel<T, ACT>), dim3(blocks + extra), dim3(256), 0, st, a, p, coef,

@@ -15,25 +15,37 @@ struct NormSizes {
   int64_t per() const { return channels / groups; }     // channels of a group
 };
 
-// Groups of a sample whose values fit here are kept in LDS as fp32, so that they are read once.
-constexpr int64_t kSlab = 8192;
-constexpr int32_t kSlabGroups = 1024;
+// Over slabs (few positions): groups of a sample are kept in LDS as fp32, so that they are read once.  A slab holds
+// kSlabAim values where it can, for several blocks on a CU (364 samples of 2408 channels in 56 groups, fp32 backward: 15
+// us, 27 with one slab of 2408), and a group of up to kSlab.  From kSlabPositions positions on the
+// split passes are faster (247 x 308 x 217 bf16, 31 groups, silu, backward: 84 us,
+// 511 over slabs).
+constexpr int64_t kSlab = 8192, kSlabAim = 2048;
+constexpr int64_t kSlabPositions = 16;
 
-// Groups of one block (0: a group does not fit, the passes are split): whole vectors of 8 channels where that
-// can be had.
+// Groups of one block (0: the passes are split): whole vectors of 8 channels where that can be had.
 inline int32_t slab_groups(const NormSizes& s) {
-  const int64_t fit = std::min<int64_t>(std::min<int64_t>(s.groups, kSlabGroups), kSlab / (s.per() * s.positions));
-  if (fit >= s.groups || fit < 1) return (int32_t)fit;
-  for (int64_t g = fit; g >= 1; --g)
+  const int64_t one = s.per() * s.positions;
+  if (s.positions >= kSlabPositions || one > kSlab) return 0;
+  const int64_t aim = std::max<int64_t>(1, kSlabAim / one), fit = kSlab / one;
+  if (aim >= s.groups) return s.groups;
+  for (int64_t g = aim; g >= 1; --g)
     if (g * s.per() % 8 == 0) return (int32_t)g;
-  return (int32_t)fit;
+  for (int64_t g = aim + 1; g <= fit && g < s.groups; ++g)
+    if (g * s.per() % 8 == 0) return (int32_t)g;
+  return (int32_t)(fit >= s.groups ? s.groups : aim);
+}
+// LDS of a block, in fp32 values.
+inline int64_t slab_values(const NormSizes& s, bool back) {
+  const int64_t gb = slab_groups(s), width = gb * s.per();
+  return back ? 2 * width * s.positions + 2 * width + 2 * gb : width * s.positions + 2 * gb;
 }
 
 // Lanes that keep a sample's group in registers (0: it has no whole vectors of 8 channels, or more than 4
 // of them a lane), and how many vectors each holds.
 inline int32_t team_lanes(const NormSizes& s) {
   const int64_t vecs = s.per() / 8 * s.positions;
-  if (s.per() % 8 != 0 || vecs > 4 * 64) return 0;
+  if (s.per() % 8 != 0 || s.positions > 4 || vecs > 4 * 64) return 0;   // (a group's rows are short pieces)
   int32_t lanes = 1;
   while (lanes < 64 && lanes < vecs) lanes *= 2;
   return lanes;
@@ -80,6 +92,10 @@ inline NormPlan plan_norm(const NormSizes& s, int64_t n) {
   p.chunks = ceil_div(s.positions, p.rows);
   return p;
 }
+
+// Whether a block joins a group's partial sums, and not a wavefront (many small ones: 7657 groups of 14 values 12
+// us by blocks, 5 by wavefronts).
+inline bool long_join(const NormSizes& s, const NormPlan& p) { return p.chunks * s.per() > 512; }
 
 // Sample ranges that the backward over slabs keeps sums of.
 inline int64_t slab_ranges(const NormSizes& s, int64_t n) {

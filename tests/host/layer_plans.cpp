@@ -49,7 +49,8 @@ static void norm_kernels(int64_t n, int64_t p, int64_t c, int32_t g, std::set<st
     snprintf(b, sizeof b, "forward slab whole=%d", slab_groups(z) == g);
     s.insert(b);
   } else {
-    s.insert("forward split");
+    snprintf(b, sizeof b, "forward split long=%d", long_join(z, plan_norm(z, n)));
+    s.insert(b);
   }
   if (lanes && p == 1) {
     snprintf(b, sizeof b, "backward team vectors=%d rows=%d", team_vectors(z), 256 / lanes / plan_team_back(z, n).groups > 1);
@@ -58,7 +59,8 @@ static void norm_kernels(int64_t n, int64_t p, int64_t c, int32_t g, std::set<st
     snprintf(b, sizeof b, "backward slab whole=%d", slab_groups(z) == g);
     s.insert(b);
   } else {
-    s.insert("backward split");
+    snprintf(b, sizeof b, "backward split long=%d", long_join(z, plan_norm(z, n)));
+    s.insert(b);
   }
 }
 
@@ -110,7 +112,7 @@ static bool bounds() {
         }
     }
   for (int64_t c : {1, 2, 8, 30, 64, 435, 2048, 5000, 65536})
-    for (int64_t p : {1, 2, 9, 100, 1000, 10000, 1000000})
+    for (int64_t p : {1, 2, 9, 15, 16, 100, 1000, 10000, 1000000})
       for (int32_t g : {1, 2, 3, 5, 8, 64, 435, 2048, 65536}) {
         if (g > c || c % g) continue;
         const NormSizes s{c, p, g};
@@ -119,6 +121,8 @@ static bool bounds() {
           for (int64_t n = 1; n <= most; n += 1 + n / 23)
             if (norm_used(s, n) > have) ok = fail("norm", c, p, g, n);
           if (norm_used(s, most) > have) ok = fail("norm", c, p, g, most);
+          if (slab_groups(s) > 0 && 4 * std::max(slab_values(s, false), slab_values(s, true)) > 159 * 1024)
+            ok = fail("norm slab", c, p, g, slab_values(s, true));
           const NormPlan q = plan_norm(s, most);
           if (q.chunks * q.rows < p || (q.chunks - 1) * q.rows >= p || q.tiles * q.col_threads * 8 < c)
             ok = fail("norm plan", c, p, g, most);
