@@ -155,10 +155,10 @@ int run_product(ot::Product p, const ot_dense* d, const ot::ProductArgs& a, ot::
   return d->precision == OT_BF16 ? ot::run_product_bf16(p, a, join, st) : ot::run_product_f32(p, a, join, st);
 }
 
-// The layer on up to 32 rows.
+// The layer straight from memory (direct_layer).
 template <class T, class Y>
 int run_rows(const ot_dense* d, const ot::RowsArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)ot::ceil_div(a.N, 16)), block(256);
+  const dim3 grid((unsigned)ot::ceil_div(a.N, 16), (unsigned)ot::ceil_div(a.M, 32)), block(256);
   if (a.M <= 16) hipLaunchKernelGGL((ot::dense_rows_kernel<T, Y, 1>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((ot::dense_rows_kernel<T, Y, 2>), grid, block, 0, st, a);
   OT_LAUNCHED("dense_rows_kernel");
@@ -257,7 +257,7 @@ extern "C" int dense_forward(ot_dense* d, const void* x, int64_t ldx, const void
   if ((rc = ot::check_device(d->device, what))) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const ot::LayerArgs ly{residual, ldr, pre, ldp, d->act, 1, 0};
-  if (ot::few_rows(e == 2, n, d->out, d->in)) {
+  if (ot::direct_layer(e == 2, n, d->out, d->in)) {
     const ot::RowsArgs a{x, ldx, w, ldw, n, d->out, d->in, bias, y, ldy, ly};
     if (e == 2) return ey == 2 ? run_rows<uint16_t, uint16_t>(d, a, st) : run_rows<uint16_t, float>(d, a, st);
     return ey == 2 ? run_rows<float, uint16_t>(d, a, st) : run_rows<float, float>(d, a, st);

@@ -1,5 +1,5 @@
-// Dense layer on few rows (a request or a small batch of them): every weight is read once and the matrix
-// instructions work straight from memory, without LDS.
+// Dense layer on few rows or few outputs (a request, a small batch, a narrow layer): the matrix instructions work
+// straight from memory, without LDS; a block takes 16 outputs of up to 32 rows.
 //
 // The weights are the first operand of a 16 x 16 product, the rows of x the second: a lane reads 16 bytes of
 // weight row n0 + l % 16 and 16 bytes of row l % 16 of x, and holds 4 neighbouring outputs 4 (l / 16) .. of one
@@ -9,7 +9,7 @@
 // Measured (us, this and the tiled products): 1, 32 rows of 2048 x 2048 bf16 7 and 15, 9 and 17; 1 row of
 // 2048 x 2048 fp32 9 and 57, of 1024 x 200000 fp32 139 and 198 (5.9 TB/s), of 65536 inputs and 64 outputs bf16
 // 76 and 347.  With more rows the loads of x, once for every 16 outputs, bound it (1000000 x 1024 bf16 on 1, 4, 16, 32
-// rows 325, 376, 515, 760, tiled 350, 351, 393, 419), so plan_rows bounds their number; a piece of x for 64
+// rows 325, 376, 515, 760, tiled 350, 351, 393, 419), so direct_layer bounds them; a piece of x for 64
 // outputs at once was no faster than the tiles (391 on 4 rows, 485 on 32).
 #pragma once
 
@@ -58,14 +58,14 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(RowsArgs a) {
   constexpr int E = 16 / sizeof(T), KS = 4, U = 8;
   __shared__ f32x4 s_acc[KS - 1][MB][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n0 = 16 * (int64_t)blockIdx.x;
+  const int64_t n0 = 16 * (int64_t)blockIdx.x, m0 = 16 * MB * (int64_t)blockIdx.y;
   const int64_t steps = (a.K + S::K - 1) / S::K, each = (steps + KS - 1) / KS;
   const int64_t k0 = min(a.K, wid * each * S::K), k1 = min(a.K, k0 + each * S::K);
   const int kl = E * (lane / 16);
   const T* w = static_cast<const T*>(a.w) + min(n0 + lane % 16, a.N - 1) * a.ldw + kl;
   const T* x[MB];
 #pragma unroll
-  for (int b = 0; b < MB; ++b) x[b] = static_cast<const T*>(a.x) + min((int64_t)16 * b + lane % 16, a.M - 1) * a.ldx + kl;
+  for (int b = 0; b < MB; ++b) x[b] = static_cast<const T*>(a.x) + min(m0 + 16 * b + lane % 16, a.M - 1) * a.ldx + kl;
   f32x4 acc[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(RowsArgs a) {
   };
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
-    const int64_t m = 16 * b + lane % 16;
+    const int64_t m = m0 + 16 * b + lane % 16;
     if (m >= a.M) continue;
     f32x4 v = acc[b];
 #pragma unroll

@@ -95,12 +95,20 @@ inline DensePlan plan_dense(bool bf16, Product product, int64_t M, int64_t N, in
 // The splits that are not empty, in whole k tiles.
 inline AdaptPlan split_dense(const DensePlan& d, int64_t K) { return split_plan(d.tile, K, d.want); }
 
-// Whether the layer runs on dense_rows.h: few rows, and so little in all that the loads of x do not count
-// (us there, and tiled: bf16 32 rows of 2048 x 2048 9, 17, of 2048 x 16384 24, 16; 8 rows of 2048 x 16384 14.7, 15,
-// of 2048 x 100000 92, 97; fp32 8, 16 rows of 1024 x 200000 175, 200 and 212, 204; 32 of 256 x 32768 14.8, 16.7).
-inline bool few_rows(bool bf16, int64_t M, int64_t N, int64_t K) {
-  if (M > 32) return false;
-  return M <= (bf16 ? 1 : 8) || M * N * K <= (1LL << (bf16 ? 28 : 29));
+// Whether the layer runs on dense_rows.h: few rows or few outputs, where the tiles are too few or walk k in too many
+// steps one after the other, and so little in all that the loads of x and W, once per 32 rows and 16 outputs,
+// do not count.  us there and tiled (rows, inputs, outputs):
+// fp32 107, 516, 1512 9.3, 21.8; 1024, 256, 256 8.2, 14.6; 256, 2048, 2048 49, 70; 1024, 2048, 16 14, 59; but 512, 516,
+//   1512 20.7, 22.7; 128, 64, 10000 10.1, 10.4; 256, 64, 10000 17.9, 12.9; 1024, 516, 1512 36, 30; and 8, 16 rows of
+//   1024, 200000 175, 200 and 212, 204;
+// bf16 32, 2048, 2048 9, 17; 64, 2048, 2048 9.8, 16.4; 128, 2048, 2048 14.9, 16.3; 1024, 2048, 16 9.6, 15.9; but 256, 2048,
+//   2048 26, 16; 256, 256, 256 9.3, 9.1; 512, 516, 1512 11.8, 9.7; 32, 2048, 16384 24, 16.
+inline bool direct_layer(bool bf16, int64_t M, int64_t N, int64_t K) {
+  if (bf16) {
+    if (M == 1 || (M <= 32 && M * N * K <= (1LL << 28))) return true;
+    return K >= 512 && M * N <= (1LL << 18) && M * N * K <= (1LL << 29);
+  }
+  return M <= 8 || (M * N <= (1LL << 19) && M * N * K <= (1LL << 30));
 }
 
 // Sums over the rows of n x cols values: a thread holds 8 columns, a block of 256 threads

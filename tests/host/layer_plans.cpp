@@ -25,8 +25,8 @@ static void dense_kernels(int64_t n, int64_t in, int64_t out, std::set<std::stri
         snprintf(b, sizeof b, "%s bf16=%d tile=%d split=%d", what, bf, a.tile, a.splits > 1);
         s.insert(b);
       };
-      if (few_rows(bf, n, out, in)) {
-        snprintf(b, sizeof b, "forward bf16=%d rows=%d", bf, n > 16);
+      if (direct_layer(bf, n, out, in)) {
+        snprintf(b, sizeof b, "forward bf16=%d direct=%d", bf, n > 32 ? 3 : n > 16 ? 2 : 1);
         s.insert(b);
       } else {
         add("forward", Product::Forward, n, out, in, 1);
