@@ -21,6 +21,8 @@
  * its leading dimension may be anything and are not written.  Vectors need
  * their elements' alignment only.
  *
+ * Outputs must not overlap each other, nor an input but where a call says that they may be the same.
+ *
  * Ownership: tensors are the caller's.  Objects hold sizes and, where said,
  * workspaces (device memory on the device current at creation, which must be
  * current in every call).  Calls are asynchronous on the given stream; calls on

@@ -27,7 +27,8 @@ struct DropoutArgs {
 };
 
 // A thread makes 8 columns of a row from one counter: ten rounds of two 32 x 32 -> 64 bit products for 8
-// values.
+// values, hidden behind the memory (640000 x 64 bf16: 28 us, 5.9 TB/s; with the loads of four rows ahead of
+// their stores, and so fewer threads on a CU, 36).
 template <class T>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a) {
   const int w = a.col_threads, lanes = 256 / w;

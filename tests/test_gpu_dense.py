@@ -267,3 +267,64 @@ def test_activations_and_slopes(name):
     assert np.isnan(got[0, 0]) and got[1, 0] == np.inf
     assert name in ("silu", "gelu") or got[2, 0] == want[2, 0]
     op.close()
+
+
+@pytest.mark.parametrize("n,n_in,n_out", [(40, 33, 50), (700, 45, 900)])
+def test_values_past_2_to_60(n, n_in, n_out):
+    """fp32 values whose bf16 terms would overflow or lose themselves keep the tolerance."""
+    rng, x, w, b = problem(n, n_in, n_out, F32, 11)
+    x[3] *= 2.0 ** 70
+    x[5, 7] = 3e37
+    w[9] *= 2.0 ** -60
+    dy = padded(rng.normal(size=(n, n_out)))
+    dy[4] *= 2.0 ** 65
+    op = layer(n_in, n_out, F32, "none", n)
+    y, dx, dw, db = like((n, n_out)), like((n, n_in)), like((n_out, n_in)), vector(np.zeros(n_out))
+    op.forward(x, w, y, bias=b)
+    op.backward(x, w, dy, dx=dx, dw=dw, dbias=db)
+    hx, hw, hdy, hb = host(x), host(w), host(dy), host(b)
+    want = ref.dense(hx, hw, hb)[0]
+    close(y, want, forward_tol(hx, hw, hb, None, want, F32, n_in)[1], "y")
+    want = ref.dense_back(hx, hw, hdy)
+    tol = backward_tols(hx, hw, hdy, None, "none", n_out, n)
+    for got, v, t in zip((dx, dw, db), want, tol):
+        close(got, v, t + U * np.abs(v))
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("name", ACTS)
+@pytest.mark.parametrize("n,n_in,n_out", [(40, 33, 50), (700, 45, 900), (600, 300, 260)])
+def test_a_gradient_that_is_not_finite_stays_in_its_row_and_column(n, n_in, n_out, name, dtype):
+    """One NaN (and, where dz is whole, one infinity) of dy: its row of dx, its row of dw, its dbias."""
+    rng, x, w, _ = problem(n, n_in, n_out, dtype, 12)
+    hp = rng.normal(size=(n, n_out))
+    hp[7, 11] = hp[9, 13] = 0.5
+    dy, pre = padded(rng.normal(size=(n, n_out)), dtype), padded(hp, dtype)
+    clean = padded(host(dy), dtype)
+    dy[7, 11] = float("nan")
+    whole = name in ("none", "relu") or dtype == F32
+    if whole:
+        dy[9, 13] = float("inf")
+    op = layer(n_in, n_out, dtype, name, n)
+    out = []
+    for g in (dy, clean):
+        dx, dw, db = like((n, n_in), dtype), like((n_out, n_in)), vector(np.zeros(n_out))
+        op.backward(x, w, g, pre=None if name == "none" else pre, dx=dx, dw=dw, dbias=db)
+        out.append([host(t) for t in (dx, dw, db)])
+    rows, cols = np.zeros(n, bool), np.zeros(n_out, bool)
+    rows[7] = cols[11] = True
+    assert np.isnan(out[0][0][7]).all() and np.isnan(out[0][1][11]).all() and np.isnan(out[0][2][11])
+    if whole:
+        rows[9] = cols[13] = True
+        with np.errstate(invalid="ignore"):
+            assert np.array_equal(out[0][0][9], np.inf * np.sign(host(w)[13]))
+            assert np.array_equal(out[0][1][13], np.inf * np.sign(host(x)[9]))
+        assert out[0][2][13] == np.inf
+    # the others' sums may be formed another way (fp32 tiles with such a value are summed again), within the tolerance
+    hx, hw, hd = host(x), host(w), host(clean)
+    tol = backward_tols(hx, hw, hd, None if name == "none" else host(pre), name, n_out, n, dtype)
+    close(out[0][0][~rows], out[1][0][~rows], 2 * tol[0][~rows] + 2 * half(dtype) * np.abs(out[1][0][~rows]), "dx")
+    close(out[0][1][~cols], out[1][1][~cols], 2 * tol[1][~cols], "dw")
+    close(out[0][2][~cols], out[1][2][~cols], 2 * tol[2][~cols], "dbias")
+    op.close()
