@@ -328,3 +328,32 @@ def test_a_gradient_that_is_not_finite_stays_in_its_row_and_column(n, n_in, n_ou
     close(out[0][1][~cols], out[1][1][~cols], 2 * tol[1][~cols], "dw")
     close(out[0][2][~cols], out[1][2][~cols], 2 * tol[2][~cols], "dbias")
     op.close()
+
+
+@pytest.mark.parametrize("name", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("n,n_in,n_out", [(300, 260, 41000), (100, 1030, 40000), (257, 256, 131072)])
+def test_long_weight_gradients(n, n_in, n_out, name):
+    """bf16 weight gradients of several rounds of blocks (ragged tiles, k with and without a rest): right in every
+    tile, and the same bits each time."""
+    rng, x, _, _ = problem(n, n_in, n_out, BF16, 13)
+    dy = padded(rng.normal(size=(n, n_out)), BF16)
+    pre = None if name == "none" else padded(rng.normal(size=(n, n_out)), BF16)
+    op = layer(n_in, n_out, BF16, name, n)
+    dw = like((n_out, n_in))
+    op.backward(x, None, dy, pre=pre, dw=dw)
+    first = dw.clone()
+    for _ in range(3):
+        dw.fill_(7.0)
+        op.backward(x, None, dy, pre=pre, dw=dw)
+        assert torch.equal(dw, first)
+    padding_kept(dw, 7.0)
+    # the 64-bit reference, some columns at a time
+    hx = host(x)
+    for c in range(0, n_out, 8192):
+        s = slice(c, min(n_out, c + 8192))
+        hd, hp = host(dy[:, s]), None if pre is None else host(pre[:, s])
+        want = ref.dense_back(hx, np.zeros((hd.shape[1], n_in)), hd, hp, name)[1]
+        a = np.abs(hd) * (1.13 if name == "gelu" else 1)
+        tol = (4 * np.sqrt(n) + 8 + (45 if name == "gelu" else 0)) * U * (a.T @ np.abs(hx))
+        close(dw[s], want, tol + U * np.abs(want), "dw")
+    op.close()
