@@ -99,11 +99,12 @@ int dense_destroy(ot_dense* d);
 
 /* channels in [1, 65536], groups dividing it, positions in [1, 2^26], eps finite and
  * above 0; max_samples: samples of the largest call that the workspaces are first
- * sized for, in [0, 2^26].  Errors: OT_E_INVAL, OT_E_NOMEM, OT_E_HIP. */
+ * sized for, in [0, 2^26], of at most 2^36 values.  Errors: OT_E_INVAL, OT_E_NOMEM,
+ * OT_E_HIP. */
 int norm_create(ot_norm** out, int64_t channels, int32_t groups, int64_t positions, int32_t precision,
                 int32_t activation, float eps, int64_t max_samples);
 
-/* n samples (0 does nothing; at most 2^40 values).  stats (nullable) receives
+/* n samples (0 does nothing; at most 2^36 values in all).  stats (nullable) receives
  * mean and rstd of every sample and group, n x groups x 2 contiguous values, for a
  * later norm_backward.  y may be x (the same address and leading dimension).
  * Errors: OT_E_INVAL, OT_E_STATE, OT_E_NOMEM, OT_E_HIP. */

@@ -52,6 +52,7 @@ struct DensePlan {
 //   256 over 1024 rows on 128 x 128 in 4, 128 x 64 in 1, 2, 4: 62, 98, 67, 59; 2048 x 2048 over 1024 on 128 x 128,
 //   128 x 64: 56, 62; 256 x 256 over 1024 on 64 x 64, 128 x 64 in 4: 13.9, 17.8.
 constexpr int64_t kLongRows = 768;
+constexpr int64_t kMostTiles = (1LL << 24) - 1;           // a launch has fewer than 2^32 threads, 256 a block
 inline DensePlan plan_dense(bool bf16, Product product, int64_t M, int64_t N, int64_t K, int planes) {
   constexpr int64_t kCUs = 256;
   auto tiles = [&](int t) { return dense_tiles(t, M, N); };
@@ -84,7 +85,7 @@ inline DensePlan plan_dense(bool bf16, Product product, int64_t M, int64_t N, in
     case Product::InputGrad:
       if (M <= 32 && N > 128) return {kF32x256, splits(2 * kCUs / tiles(kF32x256), K / 128)};
       if (M <= 64 && N > 128) return {kF64x256, splits(2 * kCUs / tiles(kF64x256), K / 128)};
-      if (M > 64 && N > 64 && K >= 1024) return {kF128x128, splits(2 * kCUs / tiles(kF128x128), K / 128)};
+      if (M > 64 && N > 64 && (K >= 1024 || tiles(kF64x64) > kMostTiles)) return {kF128x128, splits(2 * kCUs / tiles(kF128x128), K / 128)};
       return {kF64x64, splits(2 * kCUs / tiles(kF64x64), K / 64)};
     default:
       if (N > 64 && K >= kLongRows && tiles(kF128x128) >= 200) return {kF128x128, 1};

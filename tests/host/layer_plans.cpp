@@ -2,6 +2,7 @@
 //   bound            workspaces sized for n rows (samples) hold what every call of fewer needs
 //   dense            every kernel that some call takes, one a line
 //   dense-of R I O   those of the calls of a tested size (both precisions, activations with 0, 1 and 3 terms)
+//   launches         no launch of the largest calls has 2^32 threads
 //   norm, norm-of N P C G   the same for group norm
 #include <cstdio>
 #include <cstdlib>
@@ -131,10 +132,36 @@ static bool bounds() {
   return ok;
 }
 
+static bool launches() {
+  bool ok = true;
+  const int64_t most = 1LL << 36, row[] = {1, 8, 9, 31, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 513, 1000, 1023,
+                                           1024, 1025, 1029, 2047, 2049, 65535, 65537, 1 << 20, 1 << 26};
+  for (int64_t N : row)
+    for (int64_t K : {1, 40, 300, 767, 1023, 1024, 5000, 100000}) {
+      const int64_t M = std::min<int64_t>(1LL << 26, most / N);
+      for (int bf = 0; bf < 2; ++bf)
+        for (Product p : {Product::Forward, Product::InputGrad, Product::WeightGrad})
+          for (bool turn : {false, true})
+            for (int planes : {1, 2, 3}) {
+              const int64_t m = turn ? N : M, n = turn ? M : N;
+              if (p == Product::Forward && direct_layer(bf, m, n, K)) continue;
+              const DensePlan d = plan_dense(bf, p, m, n, K, planes);
+              const int64_t threads = d.tile == kT128w8 || d.tile == kT64x128 || d.tile == kT256 ? 512 : 256;
+              if (dense_tiles(d.tile, m, n) * threads >= 1LL << 32) ok = fail("dense launch", m, n, K, d.tile);
+            }
+    }
+  return ok;
+}
+
 int main(int argc, char** argv) {
   std::set<std::string> s;
   if (argc == 2 && !strcmp(argv[1], "bound")) {
     const bool ok = bounds();
+    if (ok) puts("ok");
+    return ok ? 0 : 1;
+  }
+  if (argc == 2 && !strcmp(argv[1], "launches")) {
+    const bool ok = launches();
     if (ok) puts("ok");
     return ok ? 0 : 1;
   }

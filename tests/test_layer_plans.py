@@ -38,6 +38,11 @@ def test_workspaces_cover_every_call(exe):
     assert res.returncode == 0 and res.stdout.endswith("ok\n"), res.stdout[-2000:]
 
 
+def test_launches_of_the_largest_calls(exe):
+    res = run(exe, "launches")
+    assert res.returncode == 0 and res.stdout.endswith("ok\n"), res.stdout[-2000:]
+
+
 @pytest.mark.parametrize("what,sizes", [("dense", DENSE), ("norm", NORM)])
 def test_the_gpu_tests_run_every_kernel(exe, what, sizes):
     every = set(run(exe, what).stdout.splitlines())
