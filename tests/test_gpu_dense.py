@@ -135,6 +135,30 @@ def test_a_training_pair_with_one_product(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n_in,n_out", [(77, 13), (1, 401), (2047, 1), (131, 9001)])
+def test_one_row_with_any_leading_dimension(n_in, n_out, dtype):
+    """One row may have a leading dimension that is no whole number of pieces: the same bits as padded ones."""
+    rng, x, w, b = problem(1, n_in, n_out, dtype, 8)
+    dy, pre = padded(rng.normal(size=(1, n_out)), dtype), padded(rng.normal(size=(1, n_out)), dtype)
+    r = padded(rng.normal(size=(1, n_out)), dtype)
+    op = layer(n_in, n_out, dtype, "silu", 1)
+    got = []
+    for odd in (False, True):
+        f = (lambda t: t.contiguous().as_strided(t.shape, (3, 1)) if t.shape[0] == 1 else t) if odd else lambda t: t
+        y, z, dx, dw = (f(like(s, t)) for s, t in (((1, n_out), dtype), ((1, n_out), dtype), ((1, n_in), dtype),
+                                                  ((n_out, n_in), F32)))
+        db = vector(np.zeros(n_out))
+        op.forward(f(x), f(w), y, bias=b, residual=f(r), pre=z)
+        op.backward(f(x), f(w), f(dy), pre=f(pre), dx=dx, dw=dw, dbias=db)
+        got.append((y, z, dx, dw, db))
+    for u, v in zip(*got):
+        assert torch.equal(u, v)
+    want, z = ref.dense(host(x), host(w), host(b), host(r), "silu")
+    close(got[1][0], want, forward_tol(host(x), host(w), host(b), host(r), want, dtype, n_in)[1], "y")
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_no_rows(dtype):
     op = layer(5, 9, dtype, "silu", 4)
     x, w, y = like((0, 5), dtype), like((9, 5), dtype), like((0, 9), dtype)

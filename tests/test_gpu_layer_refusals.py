@@ -158,3 +158,26 @@ def test_another_stream(ot):
         stream.synchronize()
         assert torch.equal(y, want), how
     op.close()
+
+
+def test_rows_out_of_range(ot):
+    """Numbers of rows that the headers exclude are refused before anything is read."""
+    t = torch.zeros(16, device=DEV)
+    p, st = t.data_ptr(), torch.cuda.current_stream().cuda_stream
+    dense, norm, drop = ot.DenseLayer(2048, 8, max_rows=0), ot.GroupNorm(64, 2, positions=1 << 12, max_samples=0), ot.Dropout(0.5, 1)
+    lib, e = ot.load(), ot.OT_E_INVAL
+    for n, word in ((-1, b"n outside"), ((1 << 26) + 1, b"n outside"), (1 << 26, b"2^36")):
+        assert lib.dense_forward(dense.handle, p, 2048, p, 2048, None, None, 0, n, p, 8, 0, None, 0, st) == e
+        assert word in lib.ot_last_error()
+        assert lib.dense_backward(dense.handle, p, 2048, p, 2048, n, p, 8, None, 0, p, 2048, None, 0, None, st) == e
+        assert word in lib.ot_last_error()
+        assert lib.norm_forward(norm.handle, p, 64, None, None, n, p, 64, None, st) == e
+        assert word in lib.ot_last_error()
+        assert lib.norm_backward(norm.handle, p, 64, None, None, n, p, p, 64, p, 64, None, None, st) == e
+        assert word in lib.ot_last_error()
+    for n, cols in ((-1, 4), (4, -1), (1 << 31, 4), (4, 1 << 31)):
+        assert lib.dropout_forward(drop.handle, p, 4, None, 0, n, cols, p, 4, 0, None, st) == e
+        assert lib.dropout_backward(drop.handle, p, 4, n, cols, p, 4, 0, None, st) == e
+        assert b"outside" in lib.ot_last_error()
+    for o in (dense, norm, drop):
+        o.close()
