@@ -1007,7 +1007,8 @@ __device__ __forceinline__ void layer_tail(const GemmBArgs& g, Acc (&acc)[FM][FN
 }
 
 // Layer*: a weight gradient straight from the accumulators, rows mw.. and columns nw.. of a wavefront: a store
-// writes 128 bytes of each of two rows, and no wavefront waits for another.
+// writes 128 bytes of each of two rows, and no wavefront waits for another (1000000 x 1024 over 512 rows: 1818 us, 1938
+// through LDS).
 template <int FM, int FN, class Acc>
 __device__ __forceinline__ void layer_store(const GemmBArgs& g, const Acc (&acc)[FM][FN], int64_t mw, int64_t nw,
                                             int lane) {
