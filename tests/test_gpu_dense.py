@@ -262,6 +262,42 @@ def test_row_offsets_past_32_bits(dtype):
     op.close()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_tiles_with_offsets_past_32_bits(dtype):
+    """The tiled products and the activation's backward on matrices whose rows lie 2^23 values apart, among them
+    whole k tiles past 2^32 values: the same bits as with rows that follow each other."""
+    ld, n, n_in, n_out = 1 << 23, 600, 200, 1000
+    e = 2 if dtype == BF16 else 4
+    if torch.cuda.mem_get_info()[0] < 2 * n_out * ld * e:
+        pytest.skip("not enough memory")
+    rng, x, w, b = problem(n, n_in, n_out, dtype, 14)
+    dy, r = padded(rng.normal(size=(n, n_out)), dtype), padded(rng.normal(size=(n, n_out)), dtype)
+    big = torch.empty(n_out * ld, dtype=dtype, device=DEV)
+    at = [0]
+
+    def far(t, wanted=True):
+        at[0] += 2048
+        v = torch.as_strided(big, tuple(t.shape), (ld, 1), at[0])
+        if wanted:
+            v.copy_(t)
+        return v
+
+    op = layer(n_in, n_out, dtype, "silu", n)
+    got = []
+    for place in (lambda t, wanted=True: t, far):
+        y, pre, dx = (place(like(s, dtype), False) for s in ((n, n_out), (n, n_out), (n, n_in)))
+        dw, db = like((n_out, n_in)), vector(np.zeros(n_out))
+        if place is far and dtype == F32:
+            dw = far(dw, False)
+        px, pw = place(x), place(w)
+        op.forward(px, pw, y, bias=b, residual=place(r), pre=pre)
+        op.backward(px, pw, place(dy), pre=pre, dx=dx, dw=dw, dbias=db)
+        got.append([t.clone() for t in (y, pre, dx, dw, db)])
+    for u, v in zip(*got):
+        assert torch.equal(u, v)
+    op.close()
+
+
 @pytest.mark.parametrize("name", ACTS)
 def test_activations_and_slopes(name):
     """A layer of one weight 1 is the activation itself, its input gradient the slope: over the range where gelu's

@@ -205,7 +205,7 @@ def test_offsets_past_32_bits():
     view = lambda at, n, p, c: torch.as_strided(big, (n, p, c), (p * ld, ld, 1), at)
     for n, p, c, g in ((2, 9, 16, 2), (1, 17, 1000, 1)):      # one of each form
         rng = np.random.default_rng(9)
-        x, y, dy, dx = (view(at, n, p, c) for at in (0, 1024, 2048, 3072))
+        x, y, dy, dx = (view(at, n, p, c) for at in (0, 1024, 2048, 4096))
         x.copy_(torch.from_numpy(rng.normal(size=(n, p, c))))
         dy.copy_(torch.from_numpy(rng.normal(size=(n, p, c))))
         near = [t.clone() for t in (x, dy)]
