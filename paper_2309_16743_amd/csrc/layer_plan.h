@@ -151,8 +151,8 @@ inline int64_t product_values(bool bf16, Product p, int64_t M, int64_t N, int64_
   const DensePlan d = plan_dense(bf16, p, M, N, K, planes);
   return d.want > 1 ? d.want * M * ((N + 3) / 4 * 4) : 0;
 }
-// A backward's products, as dense_backward takes them.
-inline int dx_planes(const DenseSizes& d) { return std::min(2, std::max(1, d.planes)); }
+// A backward's products, as dense_backward takes them: both every term of dz.
+inline int dx_planes(const DenseSizes& d) { return std::max(1, d.planes); }
 inline int64_t dx_values(const DenseSizes& d, int64_t n) {
   return product_values(d.bf16, Product::InputGrad, n, d.in, d.out, dx_planes(d));
 }
