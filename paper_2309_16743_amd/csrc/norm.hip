@@ -180,7 +180,10 @@ __global__ __launch_bounds__(256) void norm_team_back_kernel(NormArgs a, int S, 
     load_param(a.weight, ch[i], 1.f, w[i]);
     load_param(a.bias, ch[i], 0.f, b[i]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sw[i][e] = sb[i][e] = 0.f;
+    for (int e = 0; e < 8; ++e) {
+      if (!has[i]) w[i][e] = 1.f;                        // (idle lanes join the team's sums: 0 times channel 0's infinity)
+      sw[i][e] = sb[i][e] = 0.f;
+    }
   }
   auto total = [&](float x) {
     for (int o = 1; o < S; o <<= 1) x += __shfl_xor(x, o, 64);
