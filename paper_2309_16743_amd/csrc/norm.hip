@@ -755,26 +755,27 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(NormArgs a, NormPlan p, 
 }
 
 // Sums over the rows of part[0 / 1][row][channel] in a fixed order, dweight's and dbias's (nullable): block b of
-// gradient_blocks() takes 8 channels of one of them, its threads 32 rows side by side.
+// gradient_blocks() takes 8 channels of one of them, its threads 32 rows side by side.  In 64 bits, as the other joins:
+// the rows grow with the samples, and 4096 equal ones added one by one in fp32 are off by up to 700 u of their sum.
 __device__ __forceinline__ void gradient_block(int64_t b, const float* part, int64_t rows, int64_t channels,
                                                float* dweight, float* dbias) {
-  __shared__ float s[256];
+  __shared__ double s[256];
   const int64_t tiles = (channels + 7) / 8, which = b / tiles;
   float* out = which ? dbias : dweight;
   if (!out) return;                                      // the same for the whole block
   const int lane = threadIdx.x / 8;
   const int64_t c = b % tiles * 8 + threadIdx.x % 8;
   const float* p = part + which * rows * channels + c;
-  float sum = 0.f;
+  double sum = 0.0;
   if (c < channels)
 #pragma unroll 8
-    for (int64_t k = lane; k < rows; k += 32) sum += p[k * channels];
+    for (int64_t k = lane; k < rows; k += 32) sum += (double)p[k * channels];
   s[threadIdx.x] = sum;
   for (int h = 16; h > 0; h /= 2) {
     __syncthreads();
     if (lane < h) s[threadIdx.x] += s[threadIdx.x + 8 * h];
   }
-  if (lane == 0 && c < channels) out[c] = s[threadIdx.x];
+  if (lane == 0 && c < channels) out[c] = (float)s[threadIdx.x];
 }
 __global__ __launch_bounds__(256) void norm_gradient_kernel(const float* part, int64_t rows, int64_t channels,
                                                             float* dweight, float* dbias) {
