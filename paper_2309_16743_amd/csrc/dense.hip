@@ -297,7 +297,11 @@ extern "C" int dense_backward(ot_dense* d, const void* x, int64_t ldx, const voi
     return dbias ? zero_rows(dbias, d->out, 1, d->out, st) : OT_OK;
   }
   if (!dx && !dw && !dbias) return OT_OK;
-  if ((rc = d->ws.begin(n, st, what, [&](int64_t rows) { return d->bytes(rows); }))) return rc;
+  // without dz and partial sums a call keeps nothing between its launches
+  if ((sz.planes || (dw && ot::dw_values(sz, n)) || (dx && ot::dx_values(sz, n)) ||
+       (dbias && ot::column_values(n, d->out))) &&
+      (rc = d->ws.begin(n, st, what, [&](int64_t rows) { return d->bytes(rows); })))
+    return rc;
   const int64_t ldz = sz.planes ? ot::dz_ld(sz) : lddy;
   void* dz = sz.planes ? d->ws.p : const_cast<void*>(dy);
   float* const dw_part = reinterpret_cast<float*>(d->ws.p + ot::dz_bytes(sz, n));

@@ -34,7 +34,7 @@ inline int check_device(int device, const char* what) {
 // Device memory of an object for calls of up to `rows` rows (or samples).
 struct Workspace {
   unsigned char* p = nullptr;
-  int64_t rows = 0;
+  int64_t rows = 0, size = 0;               // size: bytes at p
   bool captured = false;                    // a captured call may name p
   std::vector<unsigned char*> kept;         // replaced after such a call
 
@@ -58,20 +58,27 @@ struct Workspace {
     }
     p = q;
     rows = n;
+    size = bytes;
     return OT_OK;
   }
-  // Before a call of n rows: bytes(n) more than there is are allocated, unless the stream is under capture.
+  // Before a call of n rows that uses the workspace: bytes(n), what calls of up to n rows need, is allocated where
+  // there is less, unless the stream is under capture.
   template <class Bytes>
   int begin(int64_t n, hipStream_t st, const char* what, Bytes bytes) {
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
     OT_HIP(hipStreamIsCapturing(st, &cap));
     if (n > rows) {
-      if (cap != hipStreamCaptureStatusNone)
-        return set_error(OT_E_STATE, "%s: a call of %lld under capture, workspaces hold %lld", what, (long long)n,
-                         (long long)rows);
-      kept.reserve(kept.size() + 1);
-      const int rc = allocate(n, bytes(n), what);
-      if (rc) return rc;
+      const int64_t need = bytes(n);
+      if (need <= size) {
+        rows = n;
+      } else {
+        if (cap != hipStreamCaptureStatusNone)
+          return set_error(OT_E_STATE, "%s: a call of %lld under capture, workspaces hold %lld", what, (long long)n,
+                           (long long)rows);
+        kept.reserve(kept.size() + 1);
+        const int rc = allocate(n, need, what);
+        if (rc) return rc;
+      }
     }
     if (cap != hipStreamCaptureStatusNone) captured = true;
     return OT_OK;

@@ -1057,7 +1057,10 @@ extern "C" int norm_backward(ot_norm* d, const void* x, int64_t ldx, const float
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (n == 0) return dweight || dbias ? gradients(nullptr, 0, d->sizes.channels, dweight, dbias, st) : OT_OK;
   if (!dx && !dweight && !dbias) return OT_OK;
-  if ((rc = d->ws.begin(n, st, what, [&](int64_t k) { return d->bytes(k); }))) return rc;
+  // dx of groups that one launch holds keeps nothing
+  if ((ot::slab_groups(d->sizes) == 0 || dweight || dbias) &&
+      (rc = d->ws.begin(n, st, what, [&](int64_t k) { return d->bytes(k); })))
+    return rc;
   ot::NormArgs a = args_of(d, n);
   a.x = x;
   a.ldx = ldx;
