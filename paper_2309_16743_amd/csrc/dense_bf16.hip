@@ -29,7 +29,7 @@ hipError_t launch(int tile, const GemmBArgs& g, int64_t splits, hipStream_t st) 
   if constexpr (P != Product::Forward) {
     if (tile == kT128w8) return launch_gemm_bf16_pipe<128, 128, 64, 2, 2, LA, LB, E, 4>(g, splits, st);
   }
-  if constexpr (!(P == Product::WeightGrad && split)) {
+  if constexpr (split == (P == Product::InputGrad)) {
     if (tile == kT256) return launch_gemm_bf16_pp<4, LA, LB, E>(g, splits, st);
   }
   return hipErrorInvalidValue;

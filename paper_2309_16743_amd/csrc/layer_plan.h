@@ -69,7 +69,9 @@ inline DensePlan plan_dense(bool bf16, Product product, int64_t M, int64_t N, in
         return {kT64x64, 1};
       case Product::InputGrad:
         if (M > 64 && tiles(kT128k32) >= 2 * kCUs - 32) return {K < 512 ? kT128k32 : kT128k64, 1};
-        if (M > 128 && k >= 65536) return {kT256, ceil_div(kCUs - 16, tiles(kT256))};
+        // (where 256 x 256 would fill the card unsplit, the line above has taken all but up to 128 columns, which leave
+        // half of it empty)
+        if (M > 128 && k >= 65536 && tiles(kT256) < kCUs - 16) return {kT256, ceil_div(kCUs - 16, tiles(kT256))};
         if (M > 64 && k >= 4096) return {kT128w8, splits(ceil_div(kCUs - 16, tiles(kT128w8)), k / 1024)};
         return {kT64x128, splits(ceil_div(kCUs - 16, tiles(kT64x128)), k / 512)};
       default:
