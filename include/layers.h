@@ -60,8 +60,8 @@ enum ot_activation { OT_ACT_NONE = 0, OT_ACT_RELU = 1, OT_ACT_SILU = 2, OT_ACT_G
 /* in, out_dim in [1, 2^26]; max_rows: rows of the largest backward that the
  * workspaces are first sized for, in [0, 2^26] (0: a layer that only serves; a
  * forward needs none).  A backward's workspace holds dz where there is an activation
- * (fp32, relu in bf16: as large as dy; silu and gelu in bf16: three times) and at most
- * 0.3 GB of partial sums.  Errors: OT_E_INVAL, OT_E_NOMEM, OT_E_HIP. */
+ * (in the layer's precision, its rows padded to 8 values; silu and gelu in bf16: three times that)
+ * and at most 0.3 GB of partial sums.  Errors: OT_E_INVAL, OT_E_NOMEM, OT_E_HIP. */
 int dense_create(ot_dense** out, int64_t in, int64_t out_dim, int32_t precision, int32_t activation,
                  int64_t max_rows);
 
@@ -95,7 +95,8 @@ int dense_destroy(ot_dense* d);
  * backward:  dp = dy act'(p);  dweight = sum of dp xh;  dbias = sum of dp, both over all samples and
  *   positions;  dx = rstd (weight dp - mean(weight dp) - xh mean(weight dp xh)), means over the group.
  * weight and bias hold one value per channel; NULL: ones, zeros.  positions = 1 and
- * groups = 1 normalise whole rows.  A group's results depend on its own values only. */
+ * groups = 1 normalise whole rows.  A group's results depend on its own values only.  Squares of
+ * differences from the mean are summed in fp32 and have to stay below 2^128. */
 
 /* channels in [1, 65536], groups dividing it, positions in [1, 2^26], eps finite and
  * above 0; max_samples: samples of the largest call that the workspaces are first

@@ -652,7 +652,6 @@ __global__ __launch_bounds__(256) void norm_coef_kernel(NormArgs a, NormPlan p, 
 // What a thread of a split pass keeps of its 8 channels: with d = x - mean, p = wr d + bias (wr = weight rstd).
 struct Channels {
   float mean[8], wr[8], b[8];
-  __device__ __forceinline__ Channels() {}
   // each(e, rstd, group of the sample) for what else is wanted
   template <class Each>
   __device__ __forceinline__ Channels(const NormArgs& a, const float* stats, int64_t sample, int64_t c, Each each) {
