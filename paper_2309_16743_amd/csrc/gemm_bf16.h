@@ -1200,12 +1200,6 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
     }
   };
   typedef float f32x16 __attribute__((ext_vector_type(16)));
-  auto frag_wait = [](bf16x8 (&af)[FM], bf16x8 (&bf)[FN]) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    frag_fence_regs(af);
-    frag_fence_regs(bf);
-  };
-
   f32x16 acc[FM][FN];
 #pragma unroll
   for (int f = 0; f < FM; ++f)
@@ -1225,14 +1219,6 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
     else if (ahead == 1) OT_WAIT_VM(PER_TILE);
     else OT_WAIT_VM(0);
     lds_barrier();
-  };
-  auto load_frags = [&](int t, int kk, bf16x8 (&af)[FM], bf16x8 (&bf)[FN]) {
-    const unsigned char* sa = smem + (t % S) * STAGE_BYTES;
-    const unsigned char* sb = sa + A_CH * 16;
-#pragma unroll
-    for (int f = 0; f < FM; ++f) af[f] = stage_frag<BK>(sa, BM / 8, LA == LayB::KMajor, WM * wm + 32 * f, kk, lane);
-#pragma unroll
-    for (int h = 0; h < FN; ++h) bf[h] = stage_frag<BK>(sb, BN / 8, LB == LayB::KMajor, WN * wn + 32 * h, kk, lane);
   };
 
   // Software pipeline: the fragments of the next 16-deep step are read while
@@ -1302,41 +1288,56 @@ __global__ __launch_bounds__(128 * NWN, OCC) void gemm_bf16_pipe_kernel(GemmBArg
       if (kt + 1 < nk) step(kt + 1, a1, b1, a0, b0);
     }
   } else {
-  bf16x8 af[FM], bfr[FN];
-  if (nk > 0) {
-    tile_ready(0);
-    if (S - 1 < nk) issue(S - 1, S - 1);
-    load_frags(0, 0, af, bfr);
-    frag_wait(af, bfr);
-  }
-  for (int kt = 0; kt < nk; ++kt) {
+    // Two sets of fragments take turns and the wait stands on every path.  With one set copied from the next, the
+    // compiler put half of the copies ahead of the wait (a copy has no order against it): a fragment was read before
+    // it had arrived, now and then, and a loss differed from itself by 5e-6.
+    typedef RawFrag<LA == LayB::KMajor> FragA;
+    typedef RawFrag<LB == LayB::KMajor> FragB;
+    static_assert(KK % 2 == 0, "fragment sets");
+    FragA a[2][FM];
+    FragB b[2][FN];
+    auto load_step = [&](int t, int kk, FragA (&x)[FM], FragB (&y)[FN]) {
+      const unsigned char* sa = smem + (t % S) * STAGE_BYTES;
+      const unsigned char* sb = sa + A_CH * 16;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      bf16x8 an[FM], bn[FN];
-      const bool more = (kk + 1 < KK) || (kt + 1 < nk);
-      if (kk + 1 < KK) {
-        load_frags(kt, kk + 1, an, bn);
-      } else if (kt + 1 < nk) {
-        tile_ready(kt + 1);
-        if (kt + S < nk) issue(kt + S, kt % S);
-        load_frags(kt + 1, 0, an, bn);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      for (int f = 0; f < FM; ++f) x[f].template read<BK>(sa, BM / 8, WM * wm + 32 * f, kk, lane);
 #pragma unroll
-      for (int f = 0; f < FM; ++f)
+      for (int h = 0; h < FN; ++h) y[h].template read<BK>(sb, BN / 8, WN * wn + 32 * h, kk, lane);
+    };
+    auto landed = [](FragA (&x)[FM], FragB (&y)[FN]) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int h = 0; h < FN; ++h)
-          acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[f], bfr[h], acc[f][h], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (more) {
-        frag_wait(an, bn);
+      for (int f = 0; f < FM; ++f) x[f].fence();
 #pragma unroll
-        for (int f = 0; f < FM; ++f) af[f] = an[f];
+      for (int h = 0; h < FN; ++h) y[h].fence();
+    };
+    if (nk > 0) {
+      tile_ready(0);
+      if (S - 1 < nk) issue(S - 1, S - 1);
+      load_step(0, 0, a[0], b[0]);
+      landed(a[0], b[0]);
+    }
+    for (int kt = 0; kt < nk; ++kt) {
 #pragma unroll
-        for (int h = 0; h < FN; ++h) bfr[h] = bn[h];
+      for (int kk = 0; kk < KK; ++kk) {
+        const int now = kk % 2, next = 1 - now;
+        if (kk + 1 < KK) {
+          load_step(kt, kk + 1, a[next], b[next]);
+        } else if (kt + 1 < nk) {
+          tile_ready(kt + 1);
+          if (kt + S < nk) issue(kt + S, kt % S);
+          load_step(kt + 1, 0, a[next], b[next]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+          for (int h = 0; h < FN; ++h)
+            acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[now][f].get(), b[now][h].get(), acc[f][h], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        landed(a[next], b[next]);
       }
     }
-  }
   }
 #undef OT_WAIT_VM
   static_assert(S <= 4, "wait depth");
