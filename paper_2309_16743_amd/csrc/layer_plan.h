@@ -40,7 +40,7 @@ struct DensePlan {
 //   Few rows of a long output (4 x 1000000 x 1024) on 64 x 64, 64 x 128, 128 x 128: 371, 357, 411.
 // bf16 input gradients: 4096 x 2048 x 2048 on 64 x 128, 128 x 128 with k tiles 32, 64, 256 x 256: 57, 51, 43, 64;
 //   160000 x 256 x 256 with k tiles 32, 64 (eight wavefronts): 47, 64.  1024 x 2048 x 2048 of one plane on 64 x 128
-//   20, on 128 x 128 in 2 splits 24; of two planes 34, and 27 with eight wavefronts in 2 splits.
+//   20, on 128 x 128 in 2 splits 24; of three planes 56, and 43 with eight wavefronts in 2 splits.
 //   512 x 1024, k 1000000 on 256 x 256, 128 x 128 in 32 splits 1140, 1220; 64 x 1024, k 100000 on 64 x 128, 128 x
 //   128 in 32: 40, 42.
 // bf16 weight gradients: 1000000 x 1024 over 512 rows on 128 x 128, 256 x 256: 2030, 1860; 100000 x 1024 over 64
